@@ -43,7 +43,7 @@ def _newer(path: str, deps) -> bool:
 def _compile(src: str, force: bool, extra) -> str:
     obj = os.path.join(OBJ_DIR, os.path.basename(src)[:-4] + ".o")
     headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")]
-    headers.append(os.path.join(ROOT, "include", "cq.h"))
+    headers += [os.path.join(ROOT, "include", h) for h in ("cq.h", "cq_bench.h", "cq_paged.h")]
     if not force and _newer(obj, [src] + headers):
         return obj
     cmd = [_hipcc(), *HIP_FLAGS, *extra, "-c", src, "-o", obj]

@@ -24,15 +24,9 @@ u64 meeting_tag() {
   }
 }
 
-}  // namespace cq
-
 namespace {
-
 thread_local char g_last_error[256] = "";
-// test / benchmark switches (cq_bench.h): per thread, never touched by the product calls
-thread_local int g_kernel_path = CQ_PATH_AUTO;
-thread_local int g_decode_chunks = 0;
-thread_local bool g_alone = false, g_one_launch = false;
+}
 
 int fail(int status, const char* fmt, ...) {
   va_list ap;
@@ -41,6 +35,17 @@ int fail(int status, const char* fmt, ...) {
   va_end(ap);
   return status;
 }
+
+}  // namespace cq
+
+namespace {
+
+// test / benchmark switches (cq_bench.h): per thread, never touched by the product calls
+thread_local int g_kernel_path = CQ_PATH_AUTO;
+thread_local int g_decode_chunks = 0;
+thread_local bool g_alone = false, g_one_launch = false;
+
+using cq::fail;
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -507,7 +512,7 @@ extern "C" {
 
 int cq_version(void) { return 200; }
 
-const char* cq_last_error(void) { return g_last_error; }
+const char* cq_last_error(void) { return cq::g_last_error; }
 
 const char* cq_status_string(int status) {
   switch (status) {

@@ -12,6 +12,9 @@
 
 namespace cq {
 
+// Keeps a message for cq_last_error() of the calling thread and returns the status.
+__attribute__((format(printf, 2, 3))) int fail(int status, const char* fmt, ...);
+
 // Tokens per block-level work item of the decode pipeline.  A "chunk" is the unit of
 // split-K: every chunk produces one (m, l, acc[d]) partial of the online softmax.
 constexpr int kVisChunk = 512;
@@ -35,7 +38,7 @@ struct Workspace {
   size_t total_bytes;
 };
 
-inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
+__host__ __device__ inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 inline Workspace workspace_layout(int B, int Hq, int d, int n_vis, int n_text) {
   Workspace w;

@@ -1,0 +1,95 @@
+// Device helpers shared by the kernels of the paged 8-bit cache (paged_append.hip, paged_few.hip, paged_prompt.hip): the
+// sequences of a step, 16-bit rows, e4m3 codes.  Internal to libcq.
+#ifndef CQ_PAGED_DEVICE_H_
+#define CQ_PAGED_DEVICE_H_
+
+#include "decode_device.h"
+#include "paged_internal.h"
+
+namespace cq {
+namespace {
+
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef unsigned int v4u __attribute__((ext_vector_type(4)));
+
+// One sequence of the step as the device sees it, brought into range.
+struct Sequence {
+  int first;   // its first row
+  int n;       // rows that are served
+  int pos0;    // place of its first row in the sequence (below 0: rows of no token)
+  int len;     // tokens in the cache
+};
+__device__ inline int clamp_int(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
+__device__ inline Sequence load_sequence(const PagedBatch& s, int b) {
+  Sequence q;
+  q.first = clamp_int(s.q_start[b], 0, s.n_tokens);
+  const int rows = clamp_int(s.q_start[b + 1], q.first, s.n_tokens) - q.first;
+  q.n = rows < s.max_new ? rows : s.max_new;
+  q.len = clamp_int(s.seq_lens[b], 0, s.len_bound);
+  q.pos0 = q.len - rows;
+  return q;
+}
+
+// ---- 16-bit elements, eight of them as they lie in memory
+template <bool BF16>
+__device__ inline float widen(unsigned lo16) {
+  if constexpr (BF16) return __builtin_bit_cast(float, lo16 << 16);
+  else return (float)__builtin_bit_cast(_Float16, (unsigned short)lo16);
+}
+template <bool BF16>
+__device__ inline void widen8(v4u w, float* x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (BF16) {
+      x[2 * i] = __builtin_bit_cast(float, w[i] << 16);
+      x[2 * i + 1] = __builtin_bit_cast(float, w[i] & 0xffff0000u);
+    } else {
+      const unsigned u = w[i];       // (the builtin would read element 0 of the vector for any other)
+      const v2h h = __builtin_bit_cast(v2h, u);
+      x[2 * i] = (float)h[0];
+      x[2 * i + 1] = (float)h[1];
+    }
+  }
+}
+// round to nearest even (the compiler's conversion; NaN stays NaN)
+template <bool BF16>
+__device__ inline unsigned narrow(float x) {
+  if constexpr (BF16) return __builtin_bit_cast(unsigned short, (__bf16)x);
+  else return __builtin_bit_cast(unsigned short, (_Float16)x);
+}
+template <bool BF16>
+__device__ inline v4u narrow8(const float* x) {
+  v4u w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = narrow<BF16>(x[2 * i]) | narrow<BF16>(x[2 * i + 1]) << 16;
+  return w;
+}
+
+// ---- e4m3 codes
+// Four codes, nearest even; |x| <= 448 or NaN.
+__device__ inline unsigned code4(float a, float b, float c, float d) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+// Eight codes (two words) as fp16 times the power of two `scale`: exact for codes times 2^-15 to 2^7.
+__device__ inline v8h codes_to_half(unsigned lo, unsigned hi, float scale) {
+  const v2h a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, false);
+  const v2h b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, true);
+  const v2h c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, false);
+  const v2h d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, true);
+  return __builtin_shufflevector(__builtin_shufflevector(a, b, 0, 1, 2, 3), __builtin_shufflevector(c, d, 0, 1, 2, 3),
+                                 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// The top bit of every byte that holds a NaN code (0x7f or 0xff); no carry leaves a byte.
+__device__ inline unsigned nan_codes(unsigned w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+constexpr float kNoMax = -3.0e38f;   // running maximum before the first token: finite, below every logit
+constexpr float kLn2 = 0.6931471805599453f;
+
+}  // namespace
+}  // namespace cq
+
+#endif  // CQ_PAGED_DEVICE_H_

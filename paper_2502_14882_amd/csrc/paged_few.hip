@@ -1,0 +1,467 @@
+// Attention over the paged e4m3 cache for few query rows per KV head: single tokens, drafted ones.
+//
+// Rows: the (new token, query head) pairs of one KV head, 16 to a tile of the matrix cores.  A wave takes 64 tokens at a time:
+//     S^T = K Q^T      A = key codes as fp16 (token rows), B = queries          v_mfma_f32_16x16x32_f16
+//     p = exp2(s - m)  with the row's running maximum m and sum l
+//     O^T += V^T P^T   A = value codes as fp16 (channel rows), B = weights
+// Lane l holds, of every product's result, column (query row) l % 16.  Which token is which row of S^T is free, and is chosen such that
+// the weights a lane has computed ARE its operand of the second product: row 4 a + i of tile t is token 16 a + 4 t + i of the 64,
+// so lane group l / 16 holds the weights of the 16 tokens 16 (l / 16) .. + 15, and its piece of the values is 16
+// consecutive bytes of a channel - which is why a page has its values channel by channel.  Nothing crosses
+// lanes but the maximum, nothing passes through LDS before the end, and since a page holds at least 16 tokens all of a
+// lane's weights have one key scale and one value scale.
+//
+// Bound: HBM, 2 d bytes per token and KV head.  Each wave keeps the keys or the values of its next step in flight while it
+// works on the other (8 KB each at 128 channels).  The four waves of a workgroup take the steps in turn and join
+// their (m, l, O) in LDS; a long sequence is split over workgroups, whose partials another launch joins.
+#include "paged_device.h"
+
+namespace cq {
+namespace {
+
+constexpr int kWaves = 4;
+
+template <int D, int NT, bool BF16>
+struct Few {
+  static constexpr int kPieces = D / 64;            // 16-byte pieces of a key row that a lane loads,
+  static constexpr bool kHalfPiece = D % 64 != 0;   // and one of 8 bytes
+  static constexpr int kKeyOps = D / 32;            // products of 32 channels
+  static constexpr int kValueTiles = D / 16;
+  static constexpr bool kPair = !BF16;              // weights as pairs of fp16: below the rounding of an fp16 result
+};
+
+// Whether, and where, 16 tokens lie: lane group by lane group.
+struct Place {
+  int pid;        // page, -1: not there or behind the end
+  int offset;     // of the 16 tokens in their page
+};
+
+template <int D, int NT, bool BF16>
+__global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAttention a) {
+  using T = Few<D, NT, BF16>;
+  constexpr int kRows = 16 * NT;
+  extern __shared__ __align__(16) float s_acc[];        // [kWaves][kRows][D + 4]
+  __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
+  const PagedCacheArgs& C = a.cache;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n = lane & 15, grp = lane >> 4;
+  unsigned id = blockIdx.x;
+  const int split = (int)(id % (unsigned)a.plan.splits);
+  id /= (unsigned)a.plan.splits;
+  const int rb = (int)(id % (unsigned)a.plan.row_blocks);
+  id /= (unsigned)a.plan.row_blocks;
+  const int h = (int)(id % (unsigned)C.heads), b = (int)(id / (unsigned)C.heads);
+  const Sequence s = load_sequence(a.batch, b);
+  const int rows = s.n * a.g, r0 = rb * kRows;
+  if (r0 >= rows) return;
+  const int parts = ceil_div(ceil_div(s.len, kStep), a.plan.split_steps);      // splits of this sequence
+  if (split >= (parts > 1 ? parts : 1)) return;
+
+  // this lane's rows
+  int limit[NT], at_row[NT], at_head[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int r = r0 + 16 * t + n, i = r / a.g;
+    at_row[t] = s.first + i;
+    at_head[t] = h * a.g + (r - i * a.g);
+    limit[t] = r >= rows ? 0 : a.causal ? clamp_int(s.pos0 + i + 1, 0, s.len) : s.len;
+  }
+  // the fewest and the most tokens that a row of the workgroup sees
+  const int last_row = (r0 + kRows < rows ? r0 + kRows : rows) - 1;
+  const int lim_lo = a.causal ? clamp_int(s.pos0 + r0 / a.g + 1, 0, s.len) : s.len;
+  const int lim_hi = a.causal ? clamp_int(s.pos0 + last_row / a.g + 1, 0, s.len) : s.len;
+  const int step0 = split * a.plan.split_steps;
+  int step1 = step0 + a.plan.split_steps;
+  if (step1 > ceil_div(lim_hi, kStep)) step1 = ceil_div(lim_hi, kStep);
+
+  // queries: every row scaled by a power of two, so that its largest element lies in [2^14, 2^15)
+  v8h q[NT][T::kKeyOps];
+  float row_scale[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const uint16_t* p = static_cast<const uint16_t*>(a.q.data);
+    const bool there = r0 + 16 * t + n < rows;
+    if (there) p += at_row[t] * a.q.token_stride + at_head[t] * a.q.head_stride;
+    v4u raw[T::kKeyOps];
+    float most = 0.f;
+#pragma unroll
+    for (int j = 0; j < T::kKeyOps; ++j) {
+      const int c = j < 2 * T::kPieces ? (j / 2) * 64 + grp * 16 + (j % 2) * 8 : T::kPieces * 64 + grp * 8;
+      raw[j] = there ? *reinterpret_cast<const v4u*>(p + c) : (v4u){0, 0, 0, 0};
+      float x[8];
+      widen8<BF16>(raw[j], x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) most = fmaxf(most, __builtin_isfinite(x[i]) ? fabsf(x[i]) : 0.f);
+    }
+    most = fmaxf(most, __shfl_xor(most, 16));
+    most = fmaxf(most, __shfl_xor(most, 32));
+    const int e = most > 0x1p-100f ? (int)(__builtin_bit_cast(unsigned, most) >> 23) - 127 - 14 : 0;
+    const float up = __builtin_bit_cast(float, (unsigned)(127 - e) << 23);
+    row_scale[t] = a.scale_log2 * __builtin_bit_cast(float, (unsigned)(127 + e) << 23);
+#pragma unroll
+    for (int j = 0; j < T::kKeyOps; ++j) {
+      float x[8];
+      widen8<BF16>(raw[j], x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) q[t][j][i] = (_Float16)(x[i] * up);
+    }
+  }
+
+  const int32_t* table = a.batch.page_table + (size_t)b * a.batch.max_pages;
+  auto place_of = [&](int step) {
+    const int tok = step * kStep + 16 * grp;
+    Place w;
+    w.pid = tok < s.len ? table[tok >> C.page_log2] : -1;
+    if ((unsigned)w.pid >= (unsigned)C.n_pages) w.pid = -1;
+    w.offset = tok & (C.page - 1);
+    return w;
+  };
+  v4u key[4][T::kPieces > 0 ? T::kPieces : 1];
+  v2u key_half[4];
+  v4u val[T::kValueTiles];
+  float key_scale, val_scale, next_key_scale = 1.f, next_val_scale = 1.f;
+  auto load_keys = [&](const Place& w) {
+    // row n of tile t is token 4 t + n % 4 of lane group n / 4
+    const int pid = __shfl(w.pid, 16 * (n >> 2)), offset = __shfl(w.offset, 16 * (n >> 2));
+    const uint8_t* p = C.k_codes + ((((size_t)(pid < 0 ? 0 : pid) * C.heads + h) << C.page_log2) + offset + (n & 3)) * D;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+      for (int j = 0; j < T::kPieces; ++j) key[t][j] = *reinterpret_cast<const v4u*>(p + 4 * t * D + 64 * j + 16 * grp);
+      if constexpr (T::kHalfPiece) key_half[t] = *reinterpret_cast<const v2u*>(p + 4 * t * D + 64 * T::kPieces + 8 * grp);
+    }
+  };
+  auto load_values = [&](const Place& w) {
+    const uint8_t* p = C.v_codes + ((((size_t)(w.pid < 0 ? 0 : w.pid) * C.heads + h) * D + n) << C.page_log2) + w.offset;
+#pragma unroll
+    for (int t = 0; t < T::kValueTiles; ++t) val[t] = *reinterpret_cast<const v4u*>(p + ((size_t)(16 * t) << C.page_log2));
+  };
+  auto load_scales = [&](const Place& w) {
+    const size_t i = (size_t)(w.pid < 0 ? 0 : w.pid) * C.heads + h;
+    next_key_scale = C.k_scale[i];
+    next_val_scale = w.pid < 0 ? 0.f : C.v_scale[i];     // 0 marks tokens that are not there
+  };
+
+  v4f acc[NT][T::kValueTiles];
+  float m[NT], l[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    m[t] = kNoMax;
+    l[t] = 0.f;
+#pragma unroll
+    for (int c = 0; c < T::kValueTiles; ++c) acc[t][c] = (v4f){0.f, 0.f, 0.f, 0.f};
+  }
+
+  int step = step0 + wave;
+  Place here = {-1, 0}, next = {-1, 0};
+  if (step < step1) {
+    here = place_of(step);
+    load_scales(here);
+    load_keys(here);
+    load_values(here);
+    next = place_of(step + kWaves < step1 ? step + kWaves : step);
+  }
+  for (; step < step1; step += kWaves) {
+    key_scale = next_key_scale;
+    val_scale = next_val_scale;
+    // ---- logits
+    v4f sc[NT][4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+      for (int r = 0; r < NT; ++r) sc[r][t] = (v4f){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < T::kKeyOps; ++j) {
+        v8h k8;
+        if (j < 2 * T::kPieces) k8 = codes_to_half(key[t][j / 2][2 * (j % 2)], key[t][j / 2][2 * (j % 2) + 1], 1.f);
+        else k8 = codes_to_half(key_half[t][0], key_half[t][1], 1.f);
+#pragma unroll
+        for (int r = 0; r < NT; ++r) sc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k8, q[r][j], sc[r][t], 0, 0, 0);
+      }
+    }
+    const bool more = step + kWaves < step1;
+    if (more) {
+      load_scales(next);
+      load_keys(next);
+    }
+    const bool there = here.pid >= 0;
+    const int tok = step * kStep + 16 * grp;
+#pragma unroll
+    for (int r = 0; r < NT; ++r) {
+      const float f = key_scale * row_scale[r];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) sc[r][t] *= f;
+    }
+    // ---- tokens that some row does not see
+    if (step * kStep + kStep > lim_lo || !__all(there)) {
+      // NaN codes of the values must not reach rows whose weight is 0: they are cleared, and the token's logit becomes the NaN
+      unsigned nan[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        // bytes of tokens that no row sees, or that are not there
+        const int live = there ? clamp_int(lim_hi - tok - 4 * w, 0, 4) : 0;
+        const unsigned keep = live == 4 ? 0xffffffffu : (1u << (8 * live)) - 1u;
+#pragma unroll
+        for (int c = 0; c < T::kValueTiles; ++c) {
+          unsigned x = val[c][w] & keep;
+          const unsigned bad = nan_codes(x);
+          nan[w] |= bad;
+          val[c][w] = x & ~((bad >> 7) * 0xffu);
+        }
+        nan[w] |= __shfl_xor(nan[w], 1);
+        nan[w] |= __shfl_xor(nan[w], 2);
+        nan[w] |= __shfl_xor(nan[w], 4);
+        nan[w] |= __shfl_xor(nan[w], 8);
+      }
+#pragma unroll
+      for (int r = 0; r < NT; ++r)
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (nan[t] >> (8 * i + 7) & 1) sc[r][t][i] = __builtin_nanf("");
+            if (!there || tok + 4 * t + i >= limit[r]) sc[r][t][i] = -__builtin_inff();
+          }
+    }
+    // ---- softmax
+    v8h w_hi[NT][2], w_lo[NT][2];
+#pragma unroll
+    for (int r = 0; r < NT; ++r) {
+      float top = sc[r][0][0];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[r][t][i]);
+      if (__any(top > m[r])) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float now = fmaxf(m[r], top), f = exp2_fast(m[r] - now);
+        m[r] = now;
+        l[r] *= f;
+#pragma unroll
+        for (int c = 0; c < T::kValueTiles; ++c) acc[r][c] *= f;
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float p = exp2_fast(sc[r][t][i] - m[r]);
+          l[r] += p;
+          const _Float16 hi = (_Float16)p;
+          w_hi[r][t / 2][4 * (t % 2) + i] = hi;
+          if constexpr (T::kPair) w_lo[r][t / 2][4 * (t % 2) + i] = (_Float16)(p - (float)hi);
+        }
+    }
+    // ---- values, in units of the largest scale of the 64 tokens
+    float unit = fmaxf(val_scale, __shfl_xor(val_scale, 16));
+    unit = fmaxf(unit, __shfl_xor(unit, 32));
+    const bool near = val_scale == 0.f || val_scale >= unit * 0x1p-15f;
+    if (__all(near)) {
+      const float rel = val_scale == 0.f ? 1.f : val_scale / unit;
+#pragma unroll
+      for (int c = 0; c < T::kValueTiles; ++c) {
+        const v8h v0 = codes_to_half(val[c][0], val[c][1], rel), v1 = codes_to_half(val[c][2], val[c][3], rel);
+#pragma unroll
+        for (int r = 0; r < NT; ++r) {
+          v4f o = {0.f, 0.f, 0.f, 0.f};
+          o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, w_hi[r][0], o, 0, 0, 0);
+          o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, w_hi[r][1], o, 0, 0, 0);
+          if constexpr (T::kPair) {
+            o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, w_lo[r][0], o, 0, 0, 0);
+            o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, w_lo[r][1], o, 0, 0, 0);
+          }
+          acc[r][c] += o * unit;
+        }
+      }
+    } else {
+      // pages whose scales lie too far apart for one fp16 range: lane group by lane group, the others' weights 0
+      const v8h none = {0, 0, 0, 0, 0, 0, 0, 0};
+      for (int part = 0; part < 4; ++part) {
+        const float f = __shfl(val_scale, 16 * part);
+        const bool mine = grp == part;
+#pragma unroll
+        for (int c = 0; c < T::kValueTiles; ++c) {
+          const v8h v0 = mine ? codes_to_half(val[c][0], val[c][1], 1.f) : none;
+          const v8h v1 = mine ? codes_to_half(val[c][2], val[c][3], 1.f) : none;
+#pragma unroll
+          for (int r = 0; r < NT; ++r) {
+            v4f o = {0.f, 0.f, 0.f, 0.f};
+            o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, w_hi[r][0], o, 0, 0, 0);
+            o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, w_hi[r][1], o, 0, 0, 0);
+            if constexpr (T::kPair) {
+              o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, w_lo[r][0], o, 0, 0, 0);
+              o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, w_lo[r][1], o, 0, 0, 0);
+            }
+            acc[r][c] += o * f;
+          }
+        }
+      }
+    }
+    here = next;
+    if (more) {
+      load_values(next);
+      if (step + 2 * kWaves < step1) next = place_of(step + 2 * kWaves);
+    }
+  }
+
+  // ---- the four waves' parts
+#pragma unroll
+  for (int r = 0; r < NT; ++r) {
+    l[r] += __shfl_xor(l[r], 16);
+    l[r] += __shfl_xor(l[r], 32);
+    if (grp == 0) {
+      s_m[wave][16 * r + n] = m[r];
+      s_l[wave][16 * r + n] = l[r];
+    }
+#pragma unroll
+    for (int c = 0; c < T::kValueTiles; ++c)
+      *reinterpret_cast<v4f*>(s_acc + (size_t)(wave * kRows + 16 * r + n) * (D + 4) + 16 * c + 4 * grp) = acc[r][c];
+  }
+  __syncthreads();
+  for (int i = tid; i < kRows * (D / 4); i += 256) {
+    const int r = i / (D / 4), c = 4 * (i % (D / 4));
+    if (r0 + r >= rows) break;
+    float top = s_m[0][r];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
+    float sum = 0.f;
+    v4f o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = exp2_fast(s_m[w][r] - top);
+      sum += s_l[w][r] * f;
+      o += *reinterpret_cast<const v4f*>(s_acc + (size_t)(w * kRows + r) * (D + 4) + c) * f;
+    }
+    const int i_new = (r0 + r) / a.g, hq = h * a.g + (r0 + r) - i_new * a.g;
+    const size_t row = (size_t)(s.first + i_new);
+    if (parts <= 1) {
+      const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+      uint16_t* p = static_cast<uint16_t*>(a.out.data) + row * a.out.token_stride + hq * a.out.head_stride + c;
+      *reinterpret_cast<v2u*>(p) = (v2u){narrow<BF16>(o[0] * inv) | narrow<BF16>(o[1] * inv) << 16,
+                                         narrow<BF16>(o[2] * inv) | narrow<BF16>(o[3] * inv) << 16};
+      if (a.lse && c == 0)
+        a.lse[row * a.q.heads + hq] = sum == 0.f ? -__builtin_inff() : (top + log2f(sum)) * kLn2;
+    } else {
+      const size_t part = (row * a.q.heads + hq) * a.plan.splits + split;
+      *reinterpret_cast<v4f*>(a.acc + part * D + c) = o;
+      if (c == 0) *reinterpret_cast<v2f*>(a.ml + part * 2) = (v2f){top, sum};
+    }
+  }
+}
+
+// Joins the splits of a row: a workgroup of four waves, a wave to a row, a lane to D / 64 channels.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256) combine_splits_kernel(PagedAttention a) {
+  constexpr int kPer = (D + 63) / 64;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  unsigned long long id = (unsigned long long)blockIdx.x * 4 + wave;
+  const int hq = (int)(id % (unsigned)a.q.heads);
+  id /= (unsigned)a.q.heads;
+  const int i = (int)(id % (unsigned)a.batch.max_new), b = (int)(id / (unsigned)a.batch.max_new);
+  if (b >= a.batch.batch) return;
+  const Sequence s = load_sequence(a.batch, b);
+  const int parts = ceil_div(ceil_div(s.len, kStep), a.plan.split_steps);
+  if (i >= s.n || parts <= 1) return;
+  const size_t row = (size_t)(s.first + i), first = (row * a.q.heads + hq) * a.plan.splits;
+  const v2f* ml = reinterpret_cast<const v2f*>(a.ml) + first;
+  float top = kNoMax;
+  for (int p = lane; p < parts; p += 64) top = fmaxf(top, ml[p][0]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  float sum = 0.f, o[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) o[j] = 0.f;
+#pragma unroll 4
+  for (int p = 0; p < parts; ++p) {
+    const v2f w = ml[p];
+    const float f = exp2_fast(w[0] - top);
+    sum += w[1] * f;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int c = lane + 64 * j;
+      if (D % 64 == 0 || c < D) o[j] += a.acc[(first + p) * D + c] * f;
+    }
+  }
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+  uint16_t* p = static_cast<uint16_t*>(a.out.data) + row * a.out.token_stride + hq * a.out.head_stride;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int c = lane + 64 * j;
+    if (D % 64 == 0 || c < D) p[c] = (uint16_t)narrow<BF16>(o[j] * inv);
+  }
+  if (a.lse && lane == 0) a.lse[row * a.q.heads + hq] = sum == 0.f ? -__builtin_inff() : (top + log2f(sum)) * kLn2;
+}
+
+template <int D, int NT>
+hipError_t launch_few(const PagedAttention& a, bool bf16, hipStream_t stream) {
+  const long long blocks = (long long)a.batch.batch * a.cache.heads * a.plan.row_blocks * a.plan.splits;
+  if (blocks >= 1ll << 24) return hipErrorInvalidValue;      // 2^32 threads
+  const size_t lds = (size_t)kWaves * 16 * NT * (D + 4) * sizeof(float);
+  const auto kernel = bf16 ? few_kernel<D, NT, true> : few_kernel<D, NT, false>;
+  static std::atomic<size_t> raised[2][kPagedDevices];
+  const hipError_t e = raise_lds(reinterpret_cast<const void*>(kernel), lds, raised[bf16]);
+  if (e != hipSuccess) return e;
+  kernel<<<dim3((unsigned)blocks), dim3(256), lds, stream>>>(a);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_few_d(const PagedAttention& a, bool bf16, hipStream_t stream) {
+  return a.plan.row_tiles == 1 ? launch_few<D, 1>(a, bf16, stream) : launch_few<D, 2>(a, bf16, stream);
+}
+
+template <int D>
+hipError_t launch_combine_d(const PagedAttention& a, bool bf16, hipStream_t stream) {
+  const long long rows = (long long)a.batch.batch * a.batch.max_new * a.q.heads;
+  const long long blocks = (rows + 3) / 4;
+  if (blocks >= 1ll << 24) return hipErrorInvalidValue;
+  if (bf16) combine_splits_kernel<D, true><<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(a);
+  else combine_splits_kernel<D, false><<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+#define CQ_FOR_HEAD_DIM(call)              \
+  switch (a.cache.d) {                     \
+    case 32: return call<32>(a, bf16, stream);   \
+    case 64: return call<64>(a, bf16, stream);   \
+    case 96: return call<96>(a, bf16, stream);   \
+    case 128: return call<128>(a, bf16, stream); \
+    case 160: return call<160>(a, bf16, stream); \
+    case 192: return call<192>(a, bf16, stream); \
+    case 224: return call<224>(a, bf16, stream); \
+    case 256: return call<256>(a, bf16, stream); \
+  }                                        \
+  return hipErrorInvalidValue
+
+hipError_t launch_paged_few(const PagedAttention& a, bool bf16, hipStream_t stream) { CQ_FOR_HEAD_DIM(launch_few_d); }
+hipError_t launch_paged_combine(const PagedAttention& a, bool bf16, hipStream_t stream) { CQ_FOR_HEAD_DIM(launch_combine_d); }
+
+// A workgroup per (sequence, KV head, tile of rows) and split.  Splits are of a fixed number of tokens, so that sequences of
+// different lengths have as many as they need; about kWorkgroups in all, a step for every wave at least.
+PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, int n_q_heads) {
+  constexpr long long kWorkgroups = 1024;
+  PagedPlan p;
+  const int g = n_q_heads / cache.heads;
+  const long long rows = (long long)batch.max_new * g;
+  p.row_tiles = rows > 16 ? 2 : 1;
+  const long long blocks = (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles);
+  p.row_blocks = (int)blocks;
+  const int steps = ceil_div(batch.len_bound, kStep);
+  const long long beside = (long long)batch.batch * cache.heads * blocks;
+  long long want = kWorkgroups / beside;
+  const long long most = ceil_div(steps, kWaves);
+  if (want > most) want = most;
+  if (want < 1) want = 1;
+  p.split_steps = ceil_div(steps, (int)want);
+  p.splits = ceil_div(steps, p.split_steps);
+  if (p.splits > 1) {
+    const size_t parts = (size_t)batch.n_tokens * n_q_heads * p.splits;
+    p.ws_acc_floats = (parts * 2 + 63) / 64 * 64;
+    p.ws_bytes = ((p.ws_acc_floats + parts * cache.d) * sizeof(float) + 255) / 256 * 256;
+    if (p.ws_bytes == 0) p.ws_bytes = 256;
+  }
+  return p;
+}
+
+}  // namespace cq

@@ -1,0 +1,96 @@
+// Declarations shared by the host side and the kernels of the paged 8-bit cache.  Not part of the ABI
+// (see include/cq_paged.h for that).
+#ifndef CQ_PAGED_INTERNAL_H_
+#define CQ_PAGED_INTERNAL_H_
+
+#include <atomic>
+
+#include "cq_internal.h"
+#include "cq_paged.h"
+
+namespace cq {
+
+constexpr int kStep = 64;   // tokens that the attention kernels take at a time: 16 to 64 of them lie in one page
+
+struct PagedCacheArgs {
+  uint8_t *k_codes, *v_codes;
+  float *k_scale, *v_scale;
+  int n_pages, heads, d;
+  int page, page_log2;
+};
+
+struct PagedBatch {
+  const int32_t *page_table, *seq_lens, *q_start;
+  int batch, max_pages, max_new, n_tokens;
+  int len_bound;   // min(max_len, max_pages * page)
+};
+
+struct HeadRows {
+  void* data;
+  long long token_stride, head_stride;
+  int heads;
+};
+
+struct RopeArgs {
+  const float* inv_freq;
+  const int32_t* positions;
+  int half;              // pairs; 0: nothing is turned
+  int adjacent;          // how they lie
+  float sign;            // of the angles
+  uint8_t axis_of[128];
+};
+
+// Raises a kernel's limit of dynamic LDS once per device; `raised` holds what it is on each, and only grows.
+// Concurrent callers may both raise it, which is harmless.
+constexpr int kPagedDevices = 64;
+inline hipError_t raise_lds(const void* kernel, size_t bytes, std::atomic<size_t>* raised) {
+  if (bytes <= 48 * 1024) return hipSuccess;
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  if (dev < 0 || dev >= kPagedDevices) return hipErrorInvalidDevice;
+  if (bytes <= raised[dev].load(std::memory_order_acquire)) return hipSuccess;
+  e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e != hipSuccess) return e;
+  size_t seen = raised[dev].load(std::memory_order_relaxed);
+  while (seen < bytes && !raised[dev].compare_exchange_weak(seen, bytes, std::memory_order_release)) {
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_rotate(const RopeArgs& rope, int n_tokens, int d, bool bf16, const HeadRows* in, const HeadRows* out,
+                         int n_tensors, hipStream_t stream);
+// q_in->heads == 0: no queries
+hipError_t launch_append(const PagedCacheArgs& cache, const PagedBatch& batch, bool bf16, const HeadRows& k,
+                         const HeadRows& v, const RopeArgs& rope, const HeadRows& q_in, const HeadRows& q_out,
+                         hipStream_t stream);
+
+// How the attention of a step is spread.
+struct PagedPlan {
+  int row_tiles = 1;       // kernel for few rows: tiles of 16 (query head, new token) rows per workgroup, 1 or 2
+  int row_blocks = 1;      // workgroups beside each other for the rows of a (sequence, KV head)
+  int split_steps = 1;     // steps of kStep tokens per split of a sequence
+  int splits = 1;          // of the longest sequence
+  size_t ws_acc_floats = 0;   // workspace: [m, l | acc]
+  size_t ws_bytes = 256;
+};
+PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, int n_q_heads);
+
+struct PagedAttention {
+  PagedCacheArgs cache;
+  PagedBatch batch;
+  HeadRows q, out;
+  float* lse;
+  int g;                   // query heads per KV head
+  int causal;
+  float scale_log2;        // softmax scale times log2(e)
+  PagedPlan plan;
+  float* ml;               // [rows][splits][2] partial maxima and sums
+  float* acc;              // [rows][splits][d]
+};
+hipError_t launch_paged_few(const PagedAttention& a, bool bf16, hipStream_t stream);
+hipError_t launch_paged_combine(const PagedAttention& a, bool bf16, hipStream_t stream);
+
+}  // namespace cq
+
+#endif  // CQ_PAGED_INTERNAL_H_

@@ -1,0 +1,454 @@
+"""The paged 8-bit cache on the GPU against its 64-bit statement (oracle/paged_oracle.py)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged_oracle as PO
+from paged_helpers import HALF_STEP, LEAST, Case, assert_attention_close
+from paper_2502_14882_amd import paged
+
+pytestmark = pytest.mark.gpu
+F16, BF16 = torch.float16, torch.bfloat16
+
+
+def run_attention(case, causal=True, scale=None, q=None, **kw):
+    cache, batch = case.device()
+    q = (case.q if q is None else q).cuda()
+    out, lse = paged.cqp_attn(cache, batch, q, causal=causal, softmax_scale=scale or 0.0, return_lse=True, **kw)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+def check_attention(case, causal=True, scale=None, pair=None):
+    out, lse = run_attention(case, causal, scale)
+    few = max(case.new) * (case.hq // case.hk) <= 32
+    assert_attention_close(out, lse, case.expected(causal, scale), case, (case.dtype == F16 and few) if pair is None else pair)
+
+
+# ---- rotation
+
+def rope_of(r, half, n_axes, pairs, lowest=1e-5):
+    freq = np.exp(r.uniform(np.log(lowest), 0, half)).astype(np.float32)
+    axis = r.randint(0, n_axes, half)
+    return freq, axis, paged.Rope(torch.from_numpy(freq).cuda(), axis, pairs, n_axes)
+
+
+@pytest.mark.parametrize("dtype", (F16, BF16))
+@pytest.mark.parametrize("pairs", (0, 1))
+@pytest.mark.parametrize("t,heads,d,rot", ((1, (1,), 32, 16), (3, (5, 2), 64, 64), (257, (7, 1), 96, 48), (70, (32, 8), 128, 128),
+                                           (33, (3,), 160, 32), (9, (2, 2), 192, 96), (5, (1, 4), 224, 224), (129, (4,), 256, 256)))
+def test_rotation(t, heads, d, rot, pairs, dtype):
+    r = np.random.RandomState(t + d)
+    n_axes = 1 + t % 4
+    freq, axis, rope = rope_of(r, rot // 2, n_axes, pairs)
+    pos = r.randint(-(1 << 31), 1 << 31, (n_axes, t)) >> r.randint(0, 31, (n_axes, t))
+    x = [torch.from_numpy(r.standard_normal((t, h, d)).astype(np.float32)).to(dtype) for h in heads]
+    dev = torch.from_numpy(pos.astype(np.int32)).cuda()
+    for backward in (False, True):
+        got = paged.cqp_rotate(rope, dev, [v.cuda() for v in x], backward=backward)
+        for a, y in zip(x, got):
+            want = PO.turn(a.float().numpy(), pos, freq, axis, pairs, backward).astype(np.float64)
+            # the same roundings but for a cosine whose 64-bit value lies at the border of two fp32 (one step, 2^-23 of up to 1 times each
+            # element of the pair: below 2^-22 of the largest element), and the rounding of the result
+            tol = HALF_STEP[dtype] * np.abs(want) + LEAST[dtype] + 2.0 ** -21 * np.abs(a.float().numpy()).max()
+            assert (np.abs(y.double().cpu().numpy() - want) <= tol).all()
+            # nearly always the same bits
+            same = torch.equal(y.cpu(), torch.from_numpy(want.astype(np.float32)).to(dtype))
+            assert same or (y.cpu() != torch.from_numpy(want.astype(np.float32)).to(dtype)).double().mean() < 1e-3
+
+
+def test_rotation_in_place_of_parts_of_a_projection():
+    """Queries and keys as slices of a fused projection, turned in place: the values beside them stay."""
+    r = np.random.RandomState(5)
+    t, hq, hk, d = 21, 6, 2, 64
+    freq, axis, rope = rope_of(r, 16, 2, 0)
+    pos = r.randint(0, 1000, (2, t))
+    qkv = torch.from_numpy(r.standard_normal((t, (hq + 2 * hk) * d)).astype(np.float32)).to(BF16)
+    dev = qkv.cuda()
+    q, k = dev[:, :hq * d].view(t, hq, d), dev[:, hq * d:(hq + hk) * d].view(t, hk, d)
+    back = paged.cqp_rotate(rope, torch.from_numpy(pos.astype(np.int32)).cuda(), [q, k], out=[q, k])
+    assert back[0] is q
+    want = PO.turn(qkv.float().numpy().reshape(t, -1, d)[:, :hq + hk], pos, freq, axis, 0)
+    got = dev.cpu().view(t, -1, d)
+    assert torch.equal(got[:, :hq + hk], torch.from_numpy(want).to(BF16))
+    assert torch.equal(got[:, hq + hk:], qkv.view(t, -1, d)[:, hq + hk:])
+    # heads before tokens: [heads, tokens, d] seen as [tokens, heads, d]
+    x = torch.from_numpy(r.standard_normal((hq, t, d)).astype(np.float32)).to(F16)
+    y = paged.cqp_rotate(rope, torch.from_numpy(pos.astype(np.int32)).cuda(), x.cuda().transpose(0, 1))
+    assert torch.equal(y.cpu(), torch.from_numpy(PO.turn(x.transpose(0, 1).float().numpy(), pos, freq, axis, 0)).to(F16))
+
+
+def test_rotation_keeps_what_is_not_finite_in_its_pair():
+    freq = torch.ones(8, device="cuda")
+    x = torch.ones((2, 1, 32), dtype=F16, device="cuda")
+    x[0, 0, 3], x[1, 0, 12], x[1, 0, 20] = float("nan"), float("inf"), float("-inf")
+    y = paged.cqp_rotate(paged.Rope(freq), torch.tensor([[1, 2]], dtype=torch.int32, device="cuda"), x)
+    bad = ~torch.isfinite(y)
+    assert bad.nonzero().tolist() == [[0, 0, 3], [0, 0, 11], [1, 0, 4], [1, 0, 12], [1, 0, 20]]
+
+
+# ---- append
+
+def check_append(case, k, v, rope=None, pos=None, freq=None, axis=None, pairs=0, q=None, max_new=None):
+    """One call on the device and by the oracle, on the case's cache; returns the device's cache."""
+    cache, batch = case.device()
+    if max_new is not None:
+        batch = paged.PagedBatch(batch.page_table, batch.seq_lens, batch.q_start, max_new, batch.max_len)
+    dev_pos = None if pos is None else torch.from_numpy(pos.astype(np.int32)).cuda()
+    got_q = paged.cqp_append_kv(cache, batch, k.cuda(), v.cuda(), rope, dev_pos, None if q is None else q.cuda())
+    kx, vx = k.float().numpy(), v.float().numpy()
+    if rope is not None:
+        kx = PO.turn(kx, pos, freq, axis, pairs)
+    limit = max_new if max_new is not None else 1 << 30
+    for codes, scale, x in ((case.kc, case.ks, kx), (case.vc, case.vs, vx)):
+        PO.append(codes, scale, x, case.table, case.lens, case.q_start, limit)
+    assert np.array_equal(cache.k_scale.cpu().numpy(), case.ks, equal_nan=True)
+    assert np.array_equal(cache.v_scale.cpu().numpy(), case.vs, equal_nan=True)
+    assert PO.same_codes(cache.k_codes.cpu().numpy(), case.kc).all()
+    assert PO.same_codes(cache.v_codes.cpu().numpy().transpose(0, 1, 3, 2), case.vc).all()
+    if q is not None:
+        want = PO.turn(q.float().numpy(), pos, freq, axis, pairs)
+        assert torch.equal(got_q.cpu(), torch.from_numpy(want).to(q.dtype))
+    return cache
+
+
+def rows(r, t, h, d, dtype, gain=1.0):
+    x = r.standard_normal((t, h, d)) * gain * np.exp2(r.uniform(-2, 2, (t, h, 1)))
+    return torch.from_numpy(x.astype(np.float32)).to(dtype)
+
+
+@pytest.mark.parametrize("dtype", (F16, BF16))
+@pytest.mark.parametrize("lens,new,hk,d,page", (
+    ((1,), (1,), 1, 32, 16), ((17, 16, 15), (1, 1, 1), 2, 64, 16), ((130, 5, 64, 65), (1, 0, 2, 3), 3, 128, 64),
+    ((300, 40), (200, 40), 2, 96, 32), ((513,), (513,), 1, 128, 128), ((520, 256), (257, 256), 1, 256, 256),
+    ((70,), (69,), 2, 224, 16), ((96, 33, 1), (31, 33, 1), 1, 160, 32), ((260,), (4,), 2, 192, 256)))
+def test_append(lens, new, hk, d, page, dtype):
+    r = np.random.RandomState(len(lens) * d + page)
+    case = Case(d + page, lens, new, hk, hk, d, page, dtype, extra_rows=3)
+    freq, axis, rope = rope_of(r, d // 4 // 8 * 8, 3, page % 3 % 2)
+    pos = r.randint(0, 100000, (3, case.t))
+    check_append(case, rows(r, case.t, hk, d, dtype, 2.0 ** -3), rows(r, case.t, hk, d, dtype, 2.0 ** 8), rope, pos, freq, axis,
+                 page % 3 % 2, rows(r, case.t, 2 * hk, d, dtype))
+
+
+def test_append_token_by_token():
+    """A page filled by single tokens whose magnitudes rise and fall: growth of the scale in every place."""
+    r = np.random.RandomState(11)
+    page, d, hk = 32, 64, 2
+    case = Case(1, (0,), (0,), hk, hk, d, page, F16)
+    case.max_pages, case.table = 2, np.array([[1, 0]], np.int32)
+    for n in range(1, 50):
+        case.lens, case.new, case.q_start, case.t = [n], [1], np.array([0, 1], np.int32), 1
+        gain = 2.0 ** r.uniform(-6, 6)
+        cache = check_append(case, rows(r, 1, hk, d, F16, gain), rows(r, 1, hk, d, F16, 1 / gain))
+        case.kc, case.ks = cache.k_codes.cpu().numpy(), cache.k_scale.cpu().numpy()
+        case.vc = np.ascontiguousarray(cache.v_codes.cpu().numpy().transpose(0, 1, 3, 2))
+        case.vs = cache.v_scale.cpu().numpy()
+
+
+def test_append_of_what_is_not_finite_or_zero():
+    r = np.random.RandomState(12)
+    case = Case(2, (20, 16), (20, 16), 2, 2, 64, 16, BF16)
+    k, v = rows(r, 36, 2, 64, BF16), rows(r, 36, 2, 64, BF16)
+    k[3, 0, 5], k[4, 1, 63], v[7, 0, 0], v[35, 1, 9] = float("nan"), float("inf"), float("-inf"), float("nan")
+    k[20:36] = 0.0
+    v[16:20, 1] = float("nan")
+    k[16, 0] = 3.0e38
+    v[17, 0] = 1e-39
+    check_append(case, k, v)
+
+
+def test_append_drops_what_has_no_place():
+    """Pages that are not there, rows before a sequence's first token, rows beyond the bound, rows of no sequence."""
+    r = np.random.RandomState(13)
+    case = Case(3, (40, 10, 64), (40, 20, 30), 2, 2, 64, 16, F16, extra_rows=5)
+    case.table[0, 1], case.table[2, 3] = -1, case.n_pages
+    check_append(case, rows(r, case.t, 2, 64, F16), rows(r, case.t, 2, 64, F16), max_new=25)
+
+
+def test_append_of_strided_rows():
+    """Keys and values as parts of a fused projection, and with the heads before the tokens."""
+    r = np.random.RandomState(14)
+    hk, d, t = 3, 64, 50
+    case = Case(4, (60, 30), (30, 20), hk, hk, d, 32, BF16)
+    fused = rows(r, t, 5 * hk, d, BF16).cuda()
+    k, v = fused[:, hk:2 * hk], fused[:, 2 * hk:3 * hk].transpose(0, 1).contiguous().transpose(0, 1)
+    assert not k.is_contiguous() and not v.is_contiguous()
+    check_append(case, k.cpu(), v.cpu())        # the oracle's side, and dense rows on the device
+    want = case.kc.copy(), case.vc.copy()
+    fresh = Case(4, (60, 30), (30, 20), hk, hk, d, 32, BF16)
+    cache, batch = fresh.device()
+    paged.cqp_append_kv(cache, batch, k, v)
+    assert PO.same_codes(cache.k_codes.cpu().numpy(), want[0]).all()
+    assert PO.same_codes(cache.v_codes.cpu().numpy().transpose(0, 1, 3, 2), want[1]).all()
+
+
+# ---- attention
+
+@pytest.mark.parametrize("dtype", (F16, BF16))
+@pytest.mark.parametrize("d", (32, 64, 96, 128, 160, 192, 224, 256))
+@pytest.mark.parametrize("page,g", ((16, 1), (64, 4), (32, 20)))
+def test_attention_single_tokens(d, page, g, dtype):
+    check_attention(Case(d + page, (1, 15, 64, 65, 257, 0, 700), (1, 1, 1, 1, 1, 0, 1), 2 * g, 2, d, page, dtype, extra_rows=2))
+
+
+@pytest.mark.parametrize("dtype", (F16, BF16))
+@pytest.mark.parametrize("page", (16, 32, 64, 128, 256))
+def test_attention_pages(page, dtype):
+    check_attention(Case(page, (1000, 255, 511), (1, 1, 1), 12, 2, 128, page, dtype, normal=True))
+
+
+@pytest.mark.parametrize("causal", (True, False))
+@pytest.mark.parametrize("dtype", (F16, BF16))
+@pytest.mark.parametrize("new,lens,hq,hk,d,page", (
+    ((8, 3, 5), (8, 70, 130), 4, 1, 128, 64), ((5, 1, 2), (700, 64, 66), 6, 2, 64, 16), ((33, 1, 64), (33, 900, 300), 8, 2, 128, 32),
+    ((100,), (100,), 3, 3, 96, 16), ((130, 0, 7), (515, 33, 7), 14, 2, 64, 128), ((70,), (200,), 16, 1, 256, 64),
+    ((65, 2), (65, 129), 5, 1, 32, 16), ((40,), (300,), 4, 2, 192, 256), ((129,), (129,), 2, 2, 160, 64), ((20,), (90,), 6, 2, 224, 32)))
+def test_attention_several_new_tokens(new, lens, hq, hk, d, page, dtype, causal):
+    check_attention(Case(d + len(new), lens, new, hq, hk, d, page, dtype, extra_rows=1), causal)
+
+
+def test_attention_of_a_long_sequence_in_splits():
+    check_attention(Case(21, (20000, 3000), (1, 1), 8, 2, 64, 64, F16, normal=True))
+    check_attention(Case(22, (9000,), (2,), 4, 1, 128, 16, BF16, normal=True))
+
+
+@pytest.mark.parametrize("new", (1, 40))
+def test_rows_that_see_nothing(new):
+    """Sequences shorter than their new rows, empty ones, pages that are not there: zeros, and minus infinity."""
+    case = Case(31, (new, 0, 3, 80), (new, 0, 0, new), 4, 2, 64, 16, F16)
+    case.lens[0] = max(new // 2, 0)
+    case.table[3, :] = -1
+    check_attention(case)
+    check_attention(case, causal=False)
+    case.table[0, 0] = case.n_pages           # the first page alone is missing
+    check_attention(case)
+
+
+@pytest.mark.parametrize("dtype", (F16, BF16))
+@pytest.mark.parametrize("new", (1, 7, 60))
+def test_scales_far_apart(new, dtype):
+    """Neighbouring pages whose value scales differ by 2^12 (one fp16 range) and by 2^40 (not), the larger values at small weights."""
+    for far in (12, 40):
+        case = Case(41 + far, (16 * 9, 70), (new, min(new, 7)), 4, 2, 64, 16, dtype, normal=True)
+        r = np.random.RandomState(far)
+        case.vs[:] = np.exp2(far * r.randint(-1, 1, case.vs.shape))
+        check_attention(case)
+
+
+@pytest.mark.parametrize("new", (1, 6, 70))
+def test_nan_reaches_those_that_see_it_only(new):
+    r = np.random.RandomState(6)
+    case = Case(51, (new + 50, new + 3), (new, new), 4, 2, 64, 32, F16, normal=True)
+    clean = case.expected()
+    at = new + 50 - (new + 1) // 2 - 1                       # half of the first sequence's new rows see this token
+    pid = case.table[0, at // 32]
+    for which in ("k", "v"):
+        kc, vc = case.kc.copy(), case.vc.copy()
+        (case.kc if which == "k" else case.vc)[pid, 1, at % 32, 7] = 0x7f
+        out, lse = run_attention(case)
+        case.kc, case.vc = kc, vc
+        sees = np.zeros((case.t, 4), bool)
+        sees[[i for i in range(new) if 50 + i >= at], 2:] = True
+        out = out.cpu().double().numpy()
+        assert np.isnan(out[sees]).any(axis=-1).all()
+        assert np.isfinite(out[~sees]).all()
+        keep = ~sees
+        assert np.allclose(out[keep], clean[0][keep], rtol=4e-3, atol=2e-2 * np.abs(clean[0]).max())
+
+
+def test_extreme_queries_and_scales():
+    """Queries near the ends of their types, and a softmax scale to bring the logits back."""
+    case = Case(61, (200,), (3,), 4, 2, 64, 32, BF16, normal=True)
+    case.q = (case.q.float() * 2.0 ** 100).to(BF16)
+    case.q[0, 0] = 0.0
+    check_attention(case, scale=2.0 ** -103)
+    case = Case(62, (200,), (3,), 4, 2, 64, 32, F16, normal=True)
+    case.q = (case.q.float() * 2.0 ** -14).to(F16)           # fp16 subnormals
+    check_attention(case, scale=2.0 ** 11)
+    case.q = torch.full_like(case.q, 60000.0)
+    check_attention(case, scale=2.0 ** -17)
+
+
+def test_attention_layouts_of_queries_and_results():
+    """Queries as a part of a fused projection, results with the heads before the tokens, a workspace of the caller's; rows of
+    nobody stay as they were."""
+    case = Case(71, (300, 40), (4, 9), 8, 2, 64, 16, BF16, extra_rows=6)
+    cache, batch = case.device()
+    fused = torch.zeros((case.t, 12, 64), dtype=BF16, device="cuda")
+    fused[:, 2:10] = case.q.cuda()
+    out = torch.full((8, case.t, 64), 7.0, dtype=BF16, device="cuda")
+    lse = torch.full((case.t, 8), 3.0, device="cuda")
+    ws = torch.empty(paged.cqp_attn_workspace_bytes(cache, batch, case.t, 8), dtype=torch.uint8, device="cuda")
+    paged.cqp_attn(cache, batch, fused[:, 2:10], out=out.transpose(0, 1), lse=lse, workspace=ws)
+    assert_attention_close(out.transpose(0, 1), lse, case.expected(), case, False)
+    assert (out[:, 13:] == 7.0).all() and (lse[13:] == 3.0).all()
+
+
+def test_same_bits_every_time():
+    case = Case(81, (5000, 100), (1, 1), 8, 2, 128, 64, F16, normal=True)
+    first = run_attention(case)
+    for _ in range(3):
+        again = run_attention(case)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+def test_joining_two_caches_by_their_sums():
+    """Attention over the first 128 tokens and over the rest, joined with lse, is attention over all."""
+    case = Case(91, (300,), (1,), 4, 2, 64, 64, F16, normal=True)
+    whole, _, _, _, _ = case.expected()
+    cache, batch = case.device()
+    parts = []
+    for lo, hi in ((0, 2), (2, 5)):
+        b = paged.PagedBatch(batch.page_table[:, lo:hi].contiguous(), torch.tensor([128 if lo == 0 else 172], dtype=torch.int32, device="cuda"),
+                             batch.q_start, 1, 300)
+        parts.append(paged.cqp_attn(cache, b, case.q.cuda(), causal=False, return_lse=True))
+    w = torch.softmax(torch.stack([p[1] for p in parts]), dim=0)[..., None]
+    got = (w * torch.stack([p[0] for p in parts]).float()).sum(0).cpu().double().numpy()
+    assert np.allclose(got, whole, rtol=2e-3, atol=2e-3 * np.abs(whole).max())
+
+
+# ---- a step as it is used
+
+def reference_step(case, k, v, q, freq, axis, pos):
+    kx = PO.turn(k.float().numpy(), pos, freq, axis, 0)
+    for codes, scale, x in ((case.kc, case.ks, kx), (case.vc, case.vs, v.float().numpy())):
+        PO.append(codes, scale, x, case.table, case.lens, case.q_start)
+    turned = torch.from_numpy(PO.turn(q.float().numpy(), pos, freq, axis, 0)).to(q.dtype)
+    return turned, case.expected(q=turned)
+
+
+@pytest.mark.parametrize("dtype", (F16, BF16))
+def test_prompt_then_tokens(dtype):
+    """Prompts of three lengths appended and attended, then five single tokens of each: rotation, cache and attention together."""
+    r = np.random.RandomState(101)
+    hq, hk, d, page, prompts = 8, 2, 64, 32, (70, 1, 33)
+    freq, axis, rope = rope_of(r, 32, 3, 0)
+    case = Case(5, prompts, prompts, hq, hk, d, page, dtype)
+    case.kc[:], case.vc[:], case.ks[:], case.vs[:] = 0x7f, 0xff, np.nan, np.nan
+    case.n_pages += 6                         # pages for what is generated
+    for name, fill in (("kc", 0x7f), ("vc", 0xff), ("ks", np.nan), ("vs", np.nan)):
+        a = getattr(case, name)
+        setattr(case, name, np.concatenate([a, np.full((6,) + a.shape[1:], fill, a.dtype)]))
+    cache, _ = case.device()
+    for step in range(6):
+        new = prompts if step == 0 else (1, 1, 1)
+        if step:
+            case.lens = [n + 1 for n in case.lens]
+        case.new, case.q_start = list(new), np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+        for b, n in enumerate(case.lens):     # a page for a token that begins one
+            if step and (n - 1) % page == 0:
+                case.table[b, (n - 1) // page] = case.n_pages - 6 + b
+        case.t = int(case.q_start[-1])
+        case.q = torch.empty((case.t, hq, d), dtype=dtype)
+        k, v, q = rows(r, case.t, hk, d, dtype), rows(r, case.t, hk, d, dtype), rows(r, case.t, hq, d, dtype, 0.25)
+        pos = r.randint(0, 4096, (3, case.t))
+        turned, want = reference_step(case, k, v, q, freq, axis, pos)
+        _, batch = case.device()
+        got_q = paged.cqp_append_kv(cache, batch, k.cuda(), v.cuda(), rope, torch.from_numpy(pos.astype(np.int32)).cuda(), q.cuda())
+        out, lse = paged.cqp_attn(cache, batch, got_q, return_lse=True)
+        assert torch.equal(got_q.cpu(), turned)
+        assert PO.same_codes(cache.k_codes.cpu().numpy(), case.kc).all()
+        assert_attention_close(out, lse, want, case, dtype == F16 and step > 0)
+
+
+def test_step_recorded_once_and_replayed_while_the_sequences_grow():
+    """Lengths, positions and page table in device memory: append and attend captured once, replayed eight times, with eager
+    work and synchronizations between, every replay checked."""
+    r = np.random.RandomState(102)
+    hq, hk, d, page, dtype = 8, 2, 128, 16, F16
+    freq, axis, rope = rope_of(r, 64, 1, 0)
+    case = Case(6, (30, 47, 200), (1, 1, 1), hq, hk, d, page, dtype, extra_pages=8, normal=True)
+    case.lens = [29, 46, 199]
+    cache, batch = case.device()
+    batch = paged.PagedBatch(batch.page_table, batch.seq_lens, batch.q_start, 1, 512)
+    case.table = np.concatenate([case.table, np.full((3, 2), 1 << 29, np.int32)], axis=1)
+    free = [p for p in range(case.n_pages) if p not in set(case.table.ravel().tolist())]
+    for b, n in enumerate(case.lens):
+        case.table[b, n // page + 1:n // page + 3] = [free.pop(), free.pop()]
+    batch = paged.PagedBatch(torch.from_numpy(case.table).cuda(), batch.seq_lens, batch.q_start, 1, 512)
+    bufs = {n: torch.zeros((3, h, d), dtype=dtype, device="cuda") for n, h in (("k", hk), ("v", hk), ("q", hq), ("out", hq))}
+    pos, lse = torch.zeros((1, 3), dtype=torch.int32, device="cuda"), torch.zeros((3, hq), device="cuda")
+    ws = torch.empty(paged.cqp_attn_workspace_bytes(cache, batch, 3, hq), dtype=torch.uint8, device="cuda")
+
+    def step():
+        batch.seq_lens.add_(1)
+        turned = paged.cqp_append_kv(cache, batch, bufs["k"], bufs["v"], rope, pos, bufs["q"])
+        paged.cqp_attn(cache, batch, turned, out=bufs["out"], lse=lse, workspace=ws)
+
+    saved = [t.clone() for t in (cache.k_codes, cache.v_codes, cache.k_scale, cache.v_scale, batch.seq_lens)]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for t, s in zip((cache.k_codes, cache.v_codes, cache.k_scale, cache.v_scale, batch.seq_lens), saved):
+        t.copy_(s)
+    for n in range(8):
+        case.lens = [x + 1 for x in case.lens]
+        new = {name: rows(r, 3, bufs[name].shape[1], d, dtype, 0.25 if name == "q" else 1.0) for name in "kvq"}
+        where = r.randint(0, 1 << 20, (1, 3))
+        for name in "kvq":
+            bufs[name].copy_(new[name])
+        pos.copy_(torch.from_numpy(where.astype(np.int32)))
+        bufs["out"].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        turned, want = reference_step(case, new["k"], new["v"], new["q"], freq, axis, where)
+        assert_attention_close(bufs["out"], lse, want, case, True)
+        eager = paged.cqp_attn(cache, batch, turned.cuda())
+        assert torch.equal(eager, bufs["out"])
+
+
+def test_calls_on_another_stream():
+    case = Case(7, (3000,), (1,), 8, 2, 128, 64, F16, normal=True)
+    want = run_attention(case)
+    cache, batch = case.device()
+    q = case.q.cuda()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = paged.cqp_attn(cache, batch, q, return_lse=True)
+    side.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each, many calls without a wait between."""
+    cases = [Case(8 + i, (6000 + 300 * i,), (1,), 8, 2, 64, 32, F16, normal=True) for i in range(2)]
+    want = [run_attention(c) for c in cases]
+    held = [c.device() + (c.q.cuda(),) for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i, (cache, batch, q) in enumerate(held):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(paged.cqp_attn(cache, batch, q, return_lse=True))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(o, want[i][0]) and torch.equal(s, want[i][1]) for o, s in got[i])
+
+
+def test_a_large_cache_is_addressed_beyond_32_bits():
+    """2.2 GB of codes each: pages whose first byte lies behind 2^31."""
+    hk, d, page = 8, 128, 64
+    n_pages = (1 << 31) // (hk * d * page) + 600
+    cache = paged.alloc_cache(n_pages, hk, d, page)
+    table = torch.tensor([[n_pages - 1, n_pages - 300, 5]], dtype=torch.int32, device="cuda")
+    batch = paged.PagedBatch(table, torch.tensor([150], dtype=torch.int32, device="cuda"),
+                             torch.tensor([0, 150], dtype=torch.int32, device="cuda"), 150, 150)
+    r = np.random.RandomState(9)
+    k, v, q = rows(r, 150, hk, d, F16), rows(r, 150, hk, d, F16), rows(r, 150, hk, d, F16, 0.25)
+    paged.cqp_append_kv(cache, batch, k.cuda(), v.cuda())
+    small = Case(9, (150,), (150,), hk, hk, d, page, F16, extra_pages=0)
+    for codes, scale, x in ((small.kc, small.ks, k), (small.vc, small.vs, v)):
+        PO.append(codes, scale, x.float().numpy(), small.table, small.lens, small.q_start)
+    ids = small.table[0, :3]
+    at = table[0].long()
+    assert PO.same_codes(cache.k_codes.view(torch.uint8)[at].cpu().numpy()[:2], small.kc[ids][:2]).all()
+    got, lse = paged.cqp_attn(cache, batch, q.cuda(), return_lse=True)
+    small.q = q
+    assert_attention_close(got, lse, small.expected(), small, False)

@@ -218,7 +218,8 @@ int cqp_attn(const cqp_cache_t* cache, const cqp_batch_t* batch, int32_t n_token
   a.ml = static_cast<float*>(workspace);
   a.acc = a.ml + a.plan.ws_acc_floats;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  hipError_t e = cq::launch_paged_few(a, dtype == CQP_BF16, st);
+  hipError_t e = a.plan.prompts ? cq::launch_paged_prompt(a, dtype == CQP_BF16, st) : hipSuccess;
+  if (e == hipSuccess && a.plan.few) e = cq::launch_paged_few(a, dtype == CQP_BF16, st);
   if (e == hipSuccess && a.plan.splits > 1) e = cq::launch_paged_combine(a, dtype == CQP_BF16, st);
   return e == hipSuccess ? CQ_OK : hip_fail(e, "attention");
 }

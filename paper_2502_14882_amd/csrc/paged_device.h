@@ -84,6 +84,13 @@ __device__ inline v8h codes_to_half(unsigned lo, unsigned hi, float scale) {
 // The top bit of every byte that holds a NaN code (0x7f or 0xff); no carry leaves a byte.
 __device__ inline unsigned nan_codes(unsigned w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
+// The power of two that brings the largest magnitude of a row of queries into [2^14, 2^15): fp16 then holds all that is not 2^-28
+// of it.  1 for rows of zeros.
+__device__ inline float row_unit(float most) {
+  const int e = most > 0x1p-100f ? (int)(__builtin_bit_cast(unsigned, most) >> 23) - 127 - 14 : 0;
+  return __builtin_bit_cast(float, (unsigned)(127 - e) << 23);
+}
+
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 constexpr float kNoMax = -3.0e38f;   // running maximum before the first token: finite, below every logit

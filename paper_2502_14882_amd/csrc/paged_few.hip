@@ -45,14 +45,14 @@ __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAt
   const PagedCacheArgs& C = a.cache;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n = lane & 15, grp = lane >> 4;
   unsigned id = blockIdx.x;
-  const int split = (int)(id % (unsigned)a.plan.splits);
-  id /= (unsigned)a.plan.splits;
+  const int split = (int)(id % (unsigned)a.plan.few_splits);
+  id /= (unsigned)a.plan.few_splits;
   const int rb = (int)(id % (unsigned)a.plan.row_blocks);
   id /= (unsigned)a.plan.row_blocks;
   const int h = (int)(id % (unsigned)C.heads), b = (int)(id / (unsigned)C.heads);
   const Sequence s = load_sequence(a.batch, b);
   const int rows = s.n * a.g, r0 = rb * kRows;
-  if (r0 >= rows) return;
+  if (r0 >= rows || (a.plan.prompts && rows > kFewRows)) return;
   const int parts = ceil_div(ceil_div(s.len, kStep), a.plan.split_steps);      // splits of this sequence
   if (split >= (parts > 1 ? parts : 1)) return;
 
@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAt
   int step1 = step0 + a.plan.split_steps;
   if (step1 > ceil_div(lim_hi, kStep)) step1 = ceil_div(lim_hi, kStep);
 
-  // queries: every row scaled by a power of two, so that its largest element lies in [2^14, 2^15)
+  // queries: every row scaled by a power of two
   v8h q[NT][T::kKeyOps];
   float row_scale[NT];
 #pragma unroll
@@ -94,9 +94,8 @@ __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAt
     }
     most = fmaxf(most, __shfl_xor(most, 16));
     most = fmaxf(most, __shfl_xor(most, 32));
-    const int e = most > 0x1p-100f ? (int)(__builtin_bit_cast(unsigned, most) >> 23) - 127 - 14 : 0;
-    const float up = __builtin_bit_cast(float, (unsigned)(127 - e) << 23);
-    row_scale[t] = a.scale_log2 * __builtin_bit_cast(float, (unsigned)(127 + e) << 23);
+    const float up = row_unit(most);
+    row_scale[t] = a.scale_log2 / up;
 #pragma unroll
     for (int j = 0; j < T::kKeyOps; ++j) {
       float x[8];
@@ -359,8 +358,12 @@ __global__ void __launch_bounds__(256) combine_splits_kernel(PagedAttention a) {
   const int i = (int)(id % (unsigned)a.batch.max_new), b = (int)(id / (unsigned)a.batch.max_new);
   if (b >= a.batch.batch) return;
   const Sequence s = load_sequence(a.batch, b);
-  const int parts = ceil_div(ceil_div(s.len, kStep), a.plan.split_steps);
+  const int split_steps = a.plan.prompts && !(a.plan.few && s.n * a.g <= kFewRows) ? a.plan.prompt_split_steps : a.plan.split_steps;
+  int parts = ceil_div(ceil_div(s.len, kStep), split_steps);
   if (i >= s.n || parts <= 1) return;
+  // the parts that hold a token which the row sees
+  const int limit = a.causal ? clamp_int(s.pos0 + i + 1, 0, s.len) : s.len;
+  parts = ceil_div(ceil_div(limit, kStep), split_steps);
   const size_t row = (size_t)(s.first + i), first = (row * a.q.heads + hq) * a.plan.splits;
   const v2f* ml = reinterpret_cast<const v2f*>(a.ml) + first;
   float top = kNoMax;
@@ -393,7 +396,7 @@ __global__ void __launch_bounds__(256) combine_splits_kernel(PagedAttention a) {
 
 template <int D, int NT>
 hipError_t launch_few(const PagedAttention& a, bool bf16, hipStream_t stream) {
-  const long long blocks = (long long)a.batch.batch * a.cache.heads * a.plan.row_blocks * a.plan.splits;
+  const long long blocks = (long long)a.batch.batch * a.cache.heads * a.plan.row_blocks * a.plan.few_splits;
   if (blocks >= 1ll << 24) return hipErrorInvalidValue;      // 2^32 threads
   const size_t lds = (size_t)kWaves * 16 * NT * (D + 4) * sizeof(float);
   const auto kernel = bf16 ? few_kernel<D, NT, true> : few_kernel<D, NT, false>;
@@ -421,40 +424,54 @@ hipError_t launch_combine_d(const PagedAttention& a, bool bf16, hipStream_t stre
 
 }  // namespace
 
-#define CQ_FOR_HEAD_DIM(call)              \
-  switch (a.cache.d) {                     \
-    case 32: return call<32>(a, bf16, stream);   \
-    case 64: return call<64>(a, bf16, stream);   \
-    case 96: return call<96>(a, bf16, stream);   \
-    case 128: return call<128>(a, bf16, stream); \
-    case 160: return call<160>(a, bf16, stream); \
-    case 192: return call<192>(a, bf16, stream); \
-    case 224: return call<224>(a, bf16, stream); \
-    case 256: return call<256>(a, bf16, stream); \
-  }                                        \
-  return hipErrorInvalidValue
-
 hipError_t launch_paged_few(const PagedAttention& a, bool bf16, hipStream_t stream) { CQ_FOR_HEAD_DIM(launch_few_d); }
 hipError_t launch_paged_combine(const PagedAttention& a, bool bf16, hipStream_t stream) { CQ_FOR_HEAD_DIM(launch_combine_d); }
 
-// A workgroup per (sequence, KV head, tile of rows) and split.  Splits are of a fixed number of tokens, so that sequences of
+// Few rows: a workgroup per (sequence, KV head, tile of rows) and split.  Splits are of a fixed number of tokens, so that sequences of
 // different lengths have as many as they need; about kWorkgroups in all, a step for every wave at least.
+// Many rows (over kFewRows per KV head): a workgroup takes a block of rows over a split; a CU holds one.  The
+// fewest splits that leave the last round of workgroups at least nine tenths full are taken, or those that fill it best: each costs its
+// partial results.  In a batch some sequences can have few rows all the same, whose workgroups are those of the other kernel.
 PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, int n_q_heads) {
   constexpr long long kWorkgroups = 1024;
   PagedPlan p;
   const int g = n_q_heads / cache.heads;
   const long long rows = (long long)batch.max_new * g;
-  p.row_tiles = rows > 16 ? 2 : 1;
-  const long long blocks = (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles);
-  p.row_blocks = (int)blocks;
   const int steps = ceil_div(batch.len_bound, kStep);
-  const long long beside = (long long)batch.batch * cache.heads * blocks;
-  long long want = kWorkgroups / beside;
-  const long long most = ceil_div(steps, kWaves);
-  if (want > most) want = most;
-  if (want < 1) want = 1;
-  p.split_steps = ceil_div(steps, (int)want);
-  p.splits = ceil_div(steps, p.split_steps);
+  p.prompts = rows > kFewRows;
+  p.few = !p.prompts || (batch.batch > 1 && g <= kFewRows);
+  if (p.few) {
+    const long long few = rows < kFewRows ? rows : kFewRows;
+    p.row_tiles = few > 16 ? 2 : 1;
+    p.row_blocks = (int)((few + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
+    const long long beside = (long long)batch.batch * cache.heads * p.row_blocks;
+    long long want = kWorkgroups / beside;
+    const long long most = ceil_div(steps, 4);
+    if (want > most) want = most;
+    if (want < 1) want = 1;
+    p.split_steps = ceil_div(steps, (int)want);
+    p.few_splits = p.splits = ceil_div(steps, p.split_steps);
+  }
+  if (p.prompts) {
+    const int block = prompt_rows(cache.d);
+    p.prompt_blocks = (int)((rows + block - 1) / block);
+    const long long beside = (long long)batch.batch * cache.heads * p.prompt_blocks, cus = device_cu_count();
+    const long long most = steps / 8 < 32 ? steps / 8 : 32;
+    int best = 1;
+    double best_full = 0;
+    for (int n = 1; n <= (most > 1 ? most : 1); ++n) {
+      const long long groups = beside * n;
+      const double full = (double)groups / (double)((groups + cus - 1) / cus * cus);
+      if (full > best_full + 0.02) {
+        best = n;
+        best_full = full;
+      }
+      if (full >= 0.9) break;
+    }
+    p.prompt_split_steps = ceil_div(steps, best);
+    p.prompt_splits = ceil_div(steps, p.prompt_split_steps);
+    if (p.prompt_splits > p.splits) p.splits = p.prompt_splits;
+  }
   if (p.splits > 1) {
     const size_t parts = (size_t)batch.n_tokens * n_q_heads * p.splits;
     p.ws_acc_floats = (parts * 2 + 63) / 64 * 64;

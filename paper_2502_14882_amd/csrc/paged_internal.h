@@ -65,15 +65,23 @@ hipError_t launch_append(const PagedCacheArgs& cache, const PagedBatch& batch, b
                          const HeadRows& v, const RopeArgs& rope, const HeadRows& q_in, const HeadRows& q_out,
                          hipStream_t stream);
 
-// How the attention of a step is spread.
+// How the attention of a step is spread: sequences of at most kFewRows (new token, query head) rows per KV head go to one kernel
+// (paged_few.hip), those of more to another (paged_prompt.hip).
+constexpr int kFewRows = 32;
 struct PagedPlan {
-  int row_tiles = 1;       // kernel for few rows: tiles of 16 (query head, new token) rows per workgroup, 1 or 2
-  int row_blocks = 1;      // workgroups beside each other for the rows of a (sequence, KV head)
-  int split_steps = 1;     // steps of kStep tokens per split of a sequence
-  int splits = 1;          // of the longest sequence
-  size_t ws_acc_floats = 0;   // workspace: [m, l | acc]
+  bool prompts = false;    // sequences of more rows are possible
+  bool few = true;         // the first kernel runs
+  int row_tiles = 1;       // its tiles of 16 rows per workgroup, 1 or 2
+  int row_blocks = 1;      // its workgroups beside each other for the rows of a (sequence, KV head)
+  int split_steps = 1;     // its steps of kStep tokens per split of a sequence
+  int few_splits = 1;      // of the longest sequence
+  int prompt_blocks = 1;   // the same of the second kernel
+  int prompt_split_steps = 1, prompt_splits = 1;
+  int splits = 1;          // the larger number of splits
+  size_t ws_acc_floats = 0;   // workspace: [m, l | acc], [rows][splits] each
   size_t ws_bytes = 256;
 };
+int prompt_rows(int d);    // rows of a workgroup of the second kernel
 PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, int n_q_heads);
 
 struct PagedAttention {
@@ -89,7 +97,21 @@ struct PagedAttention {
   float* acc;              // [rows][splits][d]
 };
 hipError_t launch_paged_few(const PagedAttention& a, bool bf16, hipStream_t stream);
+hipError_t launch_paged_prompt(const PagedAttention& a, bool bf16, hipStream_t stream);
 hipError_t launch_paged_combine(const PagedAttention& a, bool bf16, hipStream_t stream);
+
+#define CQ_FOR_HEAD_DIM(call)              \
+  switch (a.cache.d) {                     \
+    case 32: return call<32>(a, bf16, stream);   \
+    case 64: return call<64>(a, bf16, stream);   \
+    case 96: return call<96>(a, bf16, stream);   \
+    case 128: return call<128>(a, bf16, stream); \
+    case 160: return call<160>(a, bf16, stream); \
+    case 192: return call<192>(a, bf16, stream); \
+    case 224: return call<224>(a, bf16, stream); \
+    case 256: return call<256>(a, bf16, stream); \
+  }                                        \
+  return hipErrorInvalidValue
 
 }  // namespace cq
 

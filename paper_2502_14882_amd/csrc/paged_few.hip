@@ -453,7 +453,7 @@ PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, 
     p.few_splits = p.splits = ceil_div(steps, p.split_steps);
   }
   if (p.prompts) {
-    const int block = prompt_rows(cache.d);
+    const int block = prompt_rows();
     p.prompt_blocks = (int)((rows + block - 1) / block);
     const long long beside = (long long)batch.batch * cache.heads * p.prompt_blocks, cus = device_cu_count();
     const long long most = steps / 8 < 32 ? steps / 8 : 32;

@@ -81,7 +81,7 @@ struct PagedPlan {
   size_t ws_acc_floats = 0;   // workspace: [m, l | acc], [rows][splits] each
   size_t ws_bytes = 256;
 };
-int prompt_rows(int d);    // rows of a workgroup of the second kernel
+int prompt_rows();         // rows of a workgroup of the second kernel
 PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, int n_q_heads);
 
 struct PagedAttention {

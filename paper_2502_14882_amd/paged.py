@@ -13,6 +13,7 @@ raised.
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import Optional, Sequence, Tuple, Union
 
 import torch
@@ -50,10 +51,35 @@ class CqpRope(ctypes.Structure):
 _fns = None
 
 
+class _Calls:
+    """The library's cqp_* functions, as function objects of their own that take every struct as an address or as packed bytes."""
+    __slots__ = ("rotate", "append_kv", "attn_workspace_bytes", "attn")
+
+    def __init__(self, L):
+        I, V, S = ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t
+        for name, result, args in (("rotate", ctypes.c_int, [V, V, I, I, I, I, V, V, I, V]),
+                                   ("append_kv", ctypes.c_int, [V, V, I, I, V, V, V, V, V, V, V]),
+                                   ("attn_workspace_bytes", S, [V, V, I, I]),
+                                   ("attn", ctypes.c_int, [V, V, I, I, V, V, V, I, ctypes.c_float, V, S, V])):
+            f = L["cqp_" + name]
+            f.restype, f.argtypes = result, args
+            setattr(self, name, f)
+
+
+_packed: Optional[_Calls] = None
+
+
+def _calls() -> _Calls:
+    global _packed
+    if _packed is None or binding._lib is None:
+        _packed = _Calls(binding.lib())
+    return _packed
+
+
 def lib():
     """The library's cqp_* functions (cq_* ones: binding.lib())."""
     global _fns
-    if _fns is None:
+    if _fns is None or binding._lib is None:
         L = binding.lib()
         P, I, V = ctypes.POINTER, ctypes.c_int32, ctypes.c_void_p
         heads, cache, batch, rope = P(CqpHeads), P(CqpCache), P(CqpBatch), P(CqpRope)
@@ -77,7 +103,7 @@ def _need(ok: bool, text: str, *args) -> None:
 class PagedCache:
     """The pages: codes float8_e4m3fn (or uint8) [n_pages, Hkv, page, d] of the keys and [n_pages, Hkv, d, page] of the values,
     scales float32 [n_pages, Hkv].  Nothing has to be cleared."""
-    __slots__ = ("k_codes", "v_codes", "k_scale", "v_scale", "n_pages", "page", "n_kv_heads", "head_dim", "device", "c")
+    __slots__ = ("k_codes", "v_codes", "k_scale", "v_scale", "n_pages", "page", "n_kv_heads", "head_dim", "device", "index", "c", "at")
 
     def __init__(self, k_codes: torch.Tensor, v_codes: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
         _need(k_codes.dim() == 4, "k_codes are %s, [n_pages, Hkv, page, d] is wanted", tuple(k_codes.shape))
@@ -96,6 +122,7 @@ class PagedCache:
         self.device = k_codes.device
         self.c = CqpCache(self.n_pages, self.page, self.n_kv_heads, self.head_dim, k_codes.data_ptr(), v_codes.data_ptr(),
                           k_scale.data_ptr(), v_scale.data_ptr())
+        self.index, self.at = k_codes.get_device(), ctypes.addressof(self.c)
 
 
 def alloc_cache(n_pages: int, n_kv_heads: int, head_dim: int, page: int = 64, device="cuda") -> PagedCache:
@@ -110,7 +137,7 @@ class PagedBatch:
     """The sequences of a step: page_table int32 [B, max_pages], seq_lens int32 [B] (tokens in the cache, the new ones
     included), q_start int32 [B + 1] (rows of the new tokens), all on the device, and the host's bounds of the new
     tokens of a sequence and of seq_lens.  The tensors' contents may change between calls (and replays)."""
-    __slots__ = ("page_table", "seq_lens", "q_start", "max_new", "max_len", "device", "c")
+    __slots__ = ("page_table", "seq_lens", "q_start", "max_new", "max_len", "device", "index", "c", "at")
 
     def __init__(self, page_table: torch.Tensor, seq_lens: torch.Tensor, q_start: torch.Tensor, max_new: int, max_len: int):
         _need(page_table.dim() == 2, "page_table is %s, [B, max_pages] is wanted", tuple(page_table.shape))
@@ -124,12 +151,13 @@ class PagedBatch:
         self.max_new, self.max_len, self.device = int(max_new), int(max_len), page_table.device
         self.c = CqpBatch(b, page_table.shape[1], self.max_new, self.max_len, page_table.data_ptr(), seq_lens.data_ptr(),
                           q_start.data_ptr())
+        self.index, self.at = page_table.get_device(), ctypes.addressof(self.c)
 
 
 class Rope:
     """Rotary frequencies: inv_freq float32 [rot_dim / 2] on the device; axis_of says which axis of the positions each of them
     belongs to (None: one axis); pairs: CQP_PAIRS_HALVES or CQP_PAIRS_ADJACENT."""
-    __slots__ = ("inv_freq", "n_axes", "device", "c")
+    __slots__ = ("inv_freq", "n_axes", "device", "index", "c", "at")
 
     def __init__(self, inv_freq: torch.Tensor, axis_of: Optional[Sequence[int]] = None, pairs: int = CQP_PAIRS_HALVES,
                  n_axes: Optional[int] = None):
@@ -142,42 +170,60 @@ class Rope:
         self.inv_freq, self.device = inv_freq, inv_freq.device
         self.n_axes = (max(axis_of) + 1 if axis_of else 1) if n_axes is None else int(n_axes)
         self.c = CqpRope(2 * half, self.n_axes, int(pairs), 0, inv_freq.data_ptr(), (ctypes.c_uint8 * 128)(*axis_of))
+        self.index, self.at = inv_freq.get_device(), ctypes.addressof(self.c)
 
 
-def _heads(t: torch.Tensor, what: str, head_dim: int, n_tokens: int, dtype, device) -> CqpHeads:
-    _need(t.dim() == 3 and t.shape[2] == head_dim and t.shape[0] == n_tokens, "%s is %s, [%d, heads, %d] is wanted", what,
-          tuple(t.shape), n_tokens, head_dim)
-    _need(t.dtype == dtype and t.device == device, "%s is %s on %s, the call's are %s on %s", what, t.dtype, t.device, dtype, device)
-    st, sh, sc = t.stride()
-    _need(sc == 1, "the channels of %s are not contiguous", what)
+# The checks run on every call, in the time the GPU could already be working: texts are only made on failure, devices are compared
+# by index, rows of heads are packed as bytes.
+
+_pack_heads = struct.Struct("PqqiI").pack            # a cqp_heads_t
+
+
+def _heads(t: torch.Tensor, what: str, head_dim: int, n_tokens: int, dtype, index: int) -> bytes:
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != head_dim or shape[0] != n_tokens:
+        raise ValueError("%s is %s, [%d, heads, %d] is wanted" % (what, tuple(shape), n_tokens, head_dim))
+    if t.dtype is not dtype or t.get_device() != index:
+        raise ValueError("%s is %s on %s, the call's are %s on GPU %d" % (what, t.dtype, t.device, dtype, index))
+    token, head, channel = t.stride()
+    if channel != 1:
+        raise ValueError("the channels of %s are not contiguous" % what)
+    heads = shape[1]
     # a dimension of one entry is never stepped over, whatever stride it has
-    return CqpHeads(t.data_ptr(), st if t.shape[0] > 1 else 0, sh if t.shape[1] > 1 else 0, t.shape[1], 0)
+    return _pack_heads(t.data_ptr(), token if n_tokens > 1 else 0, head if heads > 1 else 0, heads, 0)
 
 
 def _dtype(t: torch.Tensor) -> int:
     code = _DTYPES.get(t.dtype)
-    _need(code is not None, "elements are float16 or bfloat16, not %s", t.dtype)
+    if code is None:
+        raise ValueError("elements are float16 or bfloat16, not %s" % t.dtype)
     return code
 
 
-def _positions(positions: torch.Tensor, rope: Rope, n_tokens: int, device) -> int:
-    _need(positions.dtype == torch.int32 and positions.is_contiguous() and positions.device == device
-          and positions.numel() == rope.n_axes * n_tokens and positions.shape[-1] == n_tokens and positions.dim() <= 2,
-          "positions are %s %s, contiguous int32 [%d, %d] is wanted", positions.dtype, tuple(positions.shape), rope.n_axes, n_tokens)
-    _need(rope.device == device, "the rope's frequencies are on %s, the call's tensors on %s", rope.device, device)
+def _positions(positions: torch.Tensor, rope: Rope, n_tokens: int, index: int) -> int:
+    shape = positions.shape
+    if (positions.dtype is not torch.int32 or not positions.is_contiguous() or positions.get_device() != index
+            or (shape != (rope.n_axes, n_tokens) and not (rope.n_axes == 1 and shape == (n_tokens,)))):
+        raise ValueError("positions are %s %s on %s, contiguous int32 [%d, %d] is wanted" % (
+            positions.dtype, tuple(shape), positions.device, rope.n_axes, n_tokens))
+    if rope.index != index:
+        raise ValueError("the rope's frequencies are on %s, the call's tensors on GPU %d" % (rope.device, index))
     return positions.data_ptr()
 
 
-def _run(device, call, *args) -> None:
-    """One call on the current stream of `device`, which is made the current one for it."""
-    if device.type == "cuda":
-        if device.index is not None and device.index != torch.cuda.current_device():
-            with torch.cuda.device(device):
-                status = call(*args, torch._C._cuda_getCurrentRawStream(device.index) or None)
-        else:
-            status = call(*args, torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None)
+def _like(t: torch.Tensor) -> torch.Tensor:
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+def _run(index: int, call, *args) -> None:
+    """One call on the current stream of GPU `index`, which is made the current one for it."""
+    if index < 0:
+        raise ValueError("the tensors are on the CPU, a GPU is wanted")
+    if index == torch._C._cuda_getDevice():
+        status = call(*args, torch._C._cuda_getCurrentRawStream(index) or None)
     else:
-        raise ValueError("the tensors are on %s, a GPU is wanted" % device)
+        with torch.cuda.device(index):
+            status = call(*args, torch._C._cuda_getCurrentRawStream(index) or None)
     if status:
         binding._check(status)
 
@@ -188,21 +234,26 @@ def cqp_rotate(rope: Rope, positions: torch.Tensor, x: Union[torch.Tensor, Seque
     tokens]; backward: by the opposite angles, which takes the gradient of the result to that of x.  out: like x (x itself:
     in place), allocated here if None.  Returns out."""
     single = isinstance(x, torch.Tensor)
-    xs = [x] if single else list(x)
-    _need(1 <= len(xs) <= 2, "one or two tensors are turned at once, not %d", len(xs))
-    outs = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in xs] if out is None else [out] if single else list(out)
-    _need(len(outs) == len(xs), "%d tensors, %d results", len(xs), len(outs))
+    xs = (x,) if single else tuple(x)
+    if not 1 <= len(xs) <= 2:
+        raise ValueError("one or two tensors are turned at once, not %d" % len(xs))
+    outs = [_like(t) for t in xs] if out is None else [out] if single else list(out)
+    if len(outs) != len(xs):
+        raise ValueError("%d tensors, %d results" % (len(xs), len(outs)))
     first = xs[0]
-    _need(first.dim() == 3, "x is %s, [tokens, heads, d] is wanted", tuple(first.shape))
-    n, _, d = first.shape
-    args = [(CqpHeads * 2)(*[_heads(t, "x" if ts is xs else "out", d, n, first.dtype, first.device) for t in ts]) for ts in (xs, outs)]
-    _run(first.device, lib().cqp_rotate, ctypes.byref(rope.c), _positions(positions, rope, n, first.device), n, d, _dtype(first),
-         int(bool(backward)), args[0], args[1], len(xs))
+    shape, dtype, index = first.shape, first.dtype, first.get_device()
+    if len(shape) != 3:
+        raise ValueError("x is %s, [tokens, heads, d] is wanted" % (tuple(shape),))
+    n, _, d = shape
+    ins, res = [b"".join([_heads(t, what, d, n, dtype, index) for t in ts]) for what, ts in (("x", xs), ("out", outs))]
+    _run(index, _calls().rotate, rope.at, _positions(positions, rope, n, index), n, d, _dtype(first), 1 if backward else 0, ins, res,
+         len(xs))
     return outs[0] if single else outs
 
 
 def _check_step(cache: PagedCache, batch: PagedBatch) -> None:
-    _need(cache.device == batch.device, "the cache is on %s, the batch on %s", cache.device, batch.device)
+    if cache.index != batch.index:
+        raise ValueError("the cache is on %s, the batch on %s" % (cache.device, batch.device))
 
 
 def cqp_append_kv(cache: PagedCache, batch: PagedBatch, k: torch.Tensor, v: torch.Tensor, rope: Optional[Rope] = None,
@@ -212,25 +263,27 @@ def cqp_append_kv(cache: PagedCache, batch: PagedBatch, k: torch.Tensor, v: torc
     [tokens, Hq, d] the queries are turned in the same launch, into q_out (q itself: in place; allocated here if None), which is
     returned."""
     _check_step(cache, batch)
-    n, d, dev = k.shape[0], cache.head_dim, cache.device
-    ks, vs = _heads(k, "k", d, n, k.dtype, dev), _heads(v, "v", d, n, k.dtype, dev)
-    _need((rope is None) == (positions is None), "rope and positions go together")
-    _need(q is not None or q_out is None, "q_out without q")
-    qs = os = None
+    n, d, index, dtype = k.shape[0], cache.head_dim, cache.index, k.dtype
+    ks, vs = _heads(k, "k", d, n, dtype, index), _heads(v, "v", d, n, dtype, index)
+    if (rope is None) != (positions is None):
+        raise ValueError("rope and positions go together")
+    where = turn = qs = os = None
+    if rope is not None:
+        turn, where = rope.at, _positions(positions, rope, n, index)
     if q is not None:
-        _need(rope is not None, "queries are turned by a rope: none is given")
+        if rope is None:
+            raise ValueError("queries are turned by a rope: none is given")
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        qs, os = _heads(q, "q", d, n, k.dtype, dev), _heads(q_out, "q_out", d, n, k.dtype, dev)
-    _run(dev, lib().cqp_append_kv, ctypes.byref(cache.c), ctypes.byref(batch.c), n, _dtype(k), ctypes.byref(ks),
-         ctypes.byref(vs), ctypes.byref(rope.c) if rope is not None else None,
-         _positions(positions, rope, n, dev) if rope is not None else None,
-         ctypes.byref(qs) if qs is not None else None, ctypes.byref(os) if os is not None else None)
+            q_out = _like(q)
+        qs, os = _heads(q, "q", d, n, dtype, index), _heads(q_out, "q_out", d, n, dtype, index)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    _run(index, _calls().append_kv, cache.at, batch.at, n, _dtype(k), ks, vs, turn, where, qs, os)
     return q_out
 
 
 def cqp_attn_workspace_bytes(cache: PagedCache, batch: PagedBatch, n_tokens: int, n_q_heads: int) -> int:
-    return int(lib().cqp_attn_workspace_bytes(ctypes.byref(cache.c), ctypes.byref(batch.c), int(n_tokens), int(n_q_heads)))
+    return int(_calls().attn_workspace_bytes(cache.at, batch.at, int(n_tokens), int(n_q_heads)))
 
 
 def cqp_attn(cache: PagedCache, batch: PagedBatch, q: torch.Tensor, causal: bool = True, softmax_scale: float = 0.0,
@@ -240,23 +293,24 @@ def cqp_attn(cache: PagedCache, batch: PagedBatch, q: torch.Tensor, causal: bool
     (or lse, a float32 [tokens, Hq] to write to) the logarithms of the rows' sums of weights.  Rows behind the last sequence
     are not written (those of an `out` allocated here are undefined)."""
     _check_step(cache, batch)
-    _need(q.dim() == 3, "q is %s, [tokens, heads, d] is wanted", tuple(q.shape))
-    n, heads, d = q.shape
+    shape, dtype, index = q.shape, q.dtype, cache.index
+    if len(shape) != 3:
+        raise ValueError("q is %s, [tokens, heads, d] is wanted" % (tuple(shape),))
+    n, heads, _ = shape
+    qs = _heads(q, "q", cache.head_dim, n, dtype, index)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if lse is None and return_lse:
-        lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
+        out = _like(q)
+    os = _heads(out, "out", cache.head_dim, n, dtype, index)
     if lse is not None:
-        _need(lse.dtype == torch.float32 and lse.shape == (n, heads) and lse.is_contiguous() and lse.device == q.device,
-              "lse is a contiguous float32 [tokens, heads]")
-    dev = cache.device
-    qs, os = _heads(q, "q", cache.head_dim, n, q.dtype, dev), _heads(out, "out", cache.head_dim, n, q.dtype, dev)
-    _need(out.shape[1] == heads, "out has %d heads, q %d", out.shape[1], heads)
+        if lse.dtype is not torch.float32 or lse.shape != (n, heads) or not lse.is_contiguous() or lse.get_device() != index:
+            raise ValueError("lse is a contiguous float32 [tokens, heads] on the cache's device")
+    elif return_lse:
+        lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
+    calls = _calls()
     if workspace is None:
-        workspace = torch.empty(cqp_attn_workspace_bytes(cache, batch, n, heads), dtype=torch.uint8, device=dev)
-    else:
-        _need(workspace.device == dev and workspace.is_contiguous(), "the workspace is contiguous and on the cache's device")
-    _run(dev, lib().cqp_attn, ctypes.byref(cache.c), ctypes.byref(batch.c), n, _dtype(q), ctypes.byref(qs), ctypes.byref(os),
-         None if lse is None else lse.data_ptr(), int(bool(causal)), float(softmax_scale), workspace.data_ptr(),
-         workspace.nbytes)
+        workspace = torch.empty(calls.attn_workspace_bytes(cache.at, batch.at, n, heads), dtype=torch.uint8, device=q.device)
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError("the workspace is contiguous and on the cache's device")
+    _run(index, calls.attn, cache.at, batch.at, n, _dtype(q), qs, os, None if lse is None else lse.data_ptr(), 1 if causal else 0,
+         softmax_scale, workspace.data_ptr(), workspace.nbytes)
     return out if lse is None else (out, lse)

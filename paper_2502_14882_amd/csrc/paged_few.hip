@@ -176,7 +176,9 @@ __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAt
 #pragma unroll
         for (int r = 0; r < NT; ++r) sc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k8, q[r][j], sc[r][t], 0, 0, 0);
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_sched_barrier(0);
     const bool more = step + kWaves < step1;
     if (more) {
       load_scales(next);
@@ -222,7 +224,7 @@ __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAt
           }
     }
     // ---- softmax
-    v8h w_hi[NT][2], w_lo[NT][2];
+    v8h p_hi[NT][2], p_lo[NT][2];
 #pragma unroll
     for (int r = 0; r < NT; ++r) {
       float top = sc[r][0][0];
@@ -246,16 +248,31 @@ __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAt
           const float p = exp2_fast(sc[r][t][i] - m[r]);
           l[r] += p;
           const _Float16 hi = (_Float16)p;
-          w_hi[r][t / 2][4 * (t % 2) + i] = hi;
-          if constexpr (T::kPair) w_lo[r][t / 2][4 * (t % 2) + i] = (_Float16)(p - (float)hi);
+          p_hi[r][t / 2][4 * (t % 2) + i] = hi;
+          if constexpr (T::kPair) p_lo[r][t / 2][4 * (t % 2) + i] = (_Float16)(p - (float)hi);
         }
     }
+    __builtin_amdgcn_sched_barrier(0);
     // ---- values, in units of the largest scale of the 64 tokens
     float unit = fmaxf(val_scale, __shfl_xor(val_scale, 16));
     unit = fmaxf(unit, __shfl_xor(unit, 32));
     const bool near = val_scale == 0.f || val_scale >= unit * 0x1p-15f;
-    if (__all(near)) {
-      const float rel = val_scale == 0.f ? 1.f : val_scale / unit;
+    // pages whose scales lie too far apart for one fp16 range: lane group by lane group, the others' weights 0
+    const bool together = __all(near);
+#pragma unroll 1
+    for (int part = 0; part < (together ? 1 : 4); ++part) {
+      const float f = together ? unit : __shfl(val_scale, 16 * part);
+      float rel = together && val_scale != 0.f ? val_scale / unit : 1.f;
+      asm volatile("" : "+v"(rel));          // the values become fp16 here, and are not kept as such for the next round
+      const unsigned mine = together || grp == part ? 0xffffffffu : 0u;
+      v8h w_hi[NT][2], w_lo[NT][2];
+#pragma unroll
+      for (int r = 0; r < NT; ++r)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          w_hi[r][i] = __builtin_bit_cast(v8h, __builtin_bit_cast(v4u, p_hi[r][i]) & mine);
+          if constexpr (T::kPair) w_lo[r][i] = __builtin_bit_cast(v8h, __builtin_bit_cast(v4u, p_lo[r][i]) & mine);
+        }
 #pragma unroll
       for (int c = 0; c < T::kValueTiles; ++c) {
         const v8h v0 = codes_to_half(val[c][0], val[c][1], rel), v1 = codes_to_half(val[c][2], val[c][3], rel);
@@ -268,31 +285,9 @@ __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAt
             o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, w_lo[r][0], o, 0, 0, 0);
             o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, w_lo[r][1], o, 0, 0, 0);
           }
-          acc[r][c] += o * unit;
+          acc[r][c] += o * f;
         }
-      }
-    } else {
-      // pages whose scales lie too far apart for one fp16 range: lane group by lane group, the others' weights 0
-      const v8h none = {0, 0, 0, 0, 0, 0, 0, 0};
-      for (int part = 0; part < 4; ++part) {
-        const float f = __shfl(val_scale, 16 * part);
-        const bool mine = grp == part;
-#pragma unroll
-        for (int c = 0; c < T::kValueTiles; ++c) {
-          const v8h v0 = mine ? codes_to_half(val[c][0], val[c][1], 1.f) : none;
-          const v8h v1 = mine ? codes_to_half(val[c][2], val[c][3], 1.f) : none;
-#pragma unroll
-          for (int r = 0; r < NT; ++r) {
-            v4f o = {0.f, 0.f, 0.f, 0.f};
-            o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, w_hi[r][0], o, 0, 0, 0);
-            o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, w_hi[r][1], o, 0, 0, 0);
-            if constexpr (T::kPair) {
-              o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, w_lo[r][0], o, 0, 0, 0);
-              o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, w_lo[r][1], o, 0, 0, 0);
-            }
-            acc[r][c] += o * f;
-          }
-        }
+        if (c % 2) __builtin_amdgcn_sched_barrier(0);
       }
     }
     here = next;

@@ -3,6 +3,7 @@
 #include <cmath>
 
 #include "paged_internal.h"
+#include "decode_meet.h"
 
 namespace {
 
@@ -215,12 +216,14 @@ int cqp_attn(const cqp_cache_t* cache, const cqp_batch_t* batch, int32_t n_token
   a.g = q->n_heads / a.cache.heads;
   a.causal = causal;
   a.scale_log2 = softmax_scale * 1.44269504088896340736f;
-  a.ml = static_cast<float*>(workspace);
-  a.acc = a.ml + a.plan.ws_acc_floats;
+  a.counts = static_cast<unsigned long long*>(workspace);
+  a.tag = a.plan.few_joins ? cq::meeting_tag() : 0;
+  a.ml = static_cast<float*>(workspace) + a.plan.ws_ml_floats;
+  a.acc = static_cast<float*>(workspace) + a.plan.ws_acc_floats;
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e = a.plan.prompts ? cq::launch_paged_prompt(a, dtype == CQP_BF16, st) : hipSuccess;
   if (e == hipSuccess && a.plan.few) e = cq::launch_paged_few(a, dtype == CQP_BF16, st);
-  if (e == hipSuccess && a.plan.splits > 1) e = cq::launch_paged_combine(a, dtype == CQP_BF16, st);
+  if (e == hipSuccess && (a.plan.prompt_splits > 1 || (a.plan.few_splits > 1 && !a.plan.few_joins))) e = cq::launch_paged_combine(a, dtype == CQP_BF16, st);
   return e == hipSuccess ? CQ_OK : hip_fail(e, "attention");
 }
 

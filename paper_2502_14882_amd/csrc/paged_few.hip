@@ -15,6 +15,7 @@
 // works on the other (8 KB each at 128 channels).  The four waves of a workgroup take the steps in turn and join
 // their (m, l, O) in LDS; a long sequence is split over workgroups, whose partials another launch joins.
 #include "paged_device.h"
+#include "decode_meet.h"
 
 namespace cq {
 namespace {
@@ -36,12 +37,23 @@ struct Place {
   int offset;     // of the 16 tokens in their page
 };
 
+// Four channels of a row's result, o / sum.
+template <bool BF16>
+__device__ inline void store_result(const PagedAttention& a, size_t row, int hq, int c, v4f o, float sum, float top) {
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+  uint16_t* p = static_cast<uint16_t*>(a.out.data) + row * a.out.token_stride + hq * a.out.head_stride + c;
+  *reinterpret_cast<v2u*>(p) = (v2u){narrow<BF16>(o[0] * inv) | narrow<BF16>(o[1] * inv) << 16,
+                                     narrow<BF16>(o[2] * inv) | narrow<BF16>(o[3] * inv) << 16};
+  if (a.lse && c == 0) a.lse[row * a.q.heads + hq] = sum == 0.f ? -__builtin_inff() : (top + log2f(sum)) * kLn2;
+}
+
 template <int D, int NT, bool BF16>
 __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAttention a) {
   using T = Few<D, NT, BF16>;
   constexpr int kRows = 16 * NT;
   extern __shared__ __align__(16) float s_acc[];        // [kWaves][kRows][D + 4]
   __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
+  __shared__ bool s_last;
   const PagedCacheArgs& C = a.cache;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n = lane & 15, grp = lane >> 4;
   unsigned id = blockIdx.x;
@@ -55,6 +67,10 @@ __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAt
   if (r0 >= rows || (a.plan.prompts && rows > kFewRows)) return;
   const int parts = ceil_div(ceil_div(s.len, kStep), a.plan.split_steps);      // splits of this sequence
   if (split >= (parts > 1 ? parts : 1)) return;
+  const bool joins = parts > 1 && a.plan.few_joins;
+  u64* const count = a.counts + ((size_t)b * C.heads + h) * a.plan.row_blocks + rb;
+  u64 seen = 0;
+  if (joins && tid == 255) seen = count_open(count, a.tag);
 
   // this lane's rows
   int limit[NT], at_row[NT], at_head[NT];
@@ -105,6 +121,7 @@ __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAt
     }
   }
 
+  const bool once = C.page <= 64 && a.plan.row_blocks == 1;
   const int32_t* table = a.batch.page_table + (size_t)b * a.batch.max_pages;
   auto place_of = [&](int step) {
     const int tok = step * kStep + 16 * grp;
@@ -131,8 +148,17 @@ __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAt
   };
   auto load_values = [&](const Place& w) {
     const uint8_t* p = C.v_codes + ((((size_t)(w.pid < 0 ? 0 : w.pid) * C.heads + h) * D + n) << C.page_log2) + w.offset;
+    // non-temporal where one instruction covers whole lines and nobody else reads them: a page's channel rows of 128 bytes and more
+    // are read half by half
+    if (once) {
+      asm volatile("; once");           // (without these the compiler makes one ordinary load of the two)
 #pragma unroll
-    for (int t = 0; t < T::kValueTiles; ++t) val[t] = *reinterpret_cast<const v4u*>(p + ((size_t)(16 * t) << C.page_log2));
+      for (int t = 0; t < T::kValueTiles; ++t) val[t] = __builtin_nontemporal_load(reinterpret_cast<const v4u*>(p + ((size_t)(16 * t) << C.page_log2)));
+      asm volatile("; once");
+    } else {
+#pragma unroll
+      for (int t = 0; t < T::kValueTiles; ++t) val[t] = *reinterpret_cast<const v4u*>(p + ((size_t)(16 * t) << C.page_log2));
+    }
   };
   auto load_scales = [&](const Place& w) {
     const size_t i = (size_t)(w.pid < 0 ? 0 : w.pid) * C.heads + h;
@@ -328,18 +354,48 @@ __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAt
     const int i_new = (r0 + r) / a.g, hq = h * a.g + (r0 + r) - i_new * a.g;
     const size_t row = (size_t)(s.first + i_new);
     if (parts <= 1) {
-      const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-      uint16_t* p = static_cast<uint16_t*>(a.out.data) + row * a.out.token_stride + hq * a.out.head_stride + c;
-      *reinterpret_cast<v2u*>(p) = (v2u){narrow<BF16>(o[0] * inv) | narrow<BF16>(o[1] * inv) << 16,
-                                         narrow<BF16>(o[2] * inv) | narrow<BF16>(o[3] * inv) << 16};
-      if (a.lse && c == 0)
-        a.lse[row * a.q.heads + hq] = sum == 0.f ? -__builtin_inff() : (top + log2f(sum)) * kLn2;
+      store_result<BF16>(a, row, hq, c, o, sum, top);
     } else {
       const size_t part = (row * a.q.heads + hq) * a.plan.splits + split;
-      *reinterpret_cast<v4f*>(a.acc + part * D + c) = o;
-      if (c == 0) *reinterpret_cast<v2f*>(a.ml + part * 2) = (v2f){top, sum};
+      store_device(a.acc + part * D + c, o[0], o[1]);
+      store_device(a.acc + part * D + c + 2, o[2], o[3]);
+      if (c == 0) store_device(a.ml + part * 2, top, sum);
     }
   }
+  if (!joins) return;
+
+  // ---- the workgroup that is counted last joins the splits, in their order
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // this wave's part has reached memory
+  __syncthreads();
+  if (tid == 255) s_last = count_in(count, a.tag, seen) == parts - 1;
+  __syncthreads();
+  if (!s_last) return;
+  const int live = rows - r0 < kRows ? rows - r0 : kRows;
+  v2f* const s_ml = reinterpret_cast<v2f*>(s_acc);          // [live][parts]
+  auto first_part = [&](int r) {
+    const int i_new = (r0 + r) / a.g;
+    return ((size_t)(s.first + i_new) * a.q.heads + h * a.g + (r0 + r) - i_new * a.g) * a.plan.splits;
+  };
+  for (int i = tid; i < live * parts; i += 256) s_ml[i] = load_device(a.ml + 2 * (first_part(i / parts) + i % parts));
+  __syncthreads();
+  for (int i = tid; i < live * (D / 4); i += 256) {
+    const int r = i / (D / 4), c = 4 * (i % (D / 4));
+    const float* from = a.acc + first_part(r) * D + c;
+    const v2f* ml = s_ml + r * parts;
+    float top = kNoMax, sum = 0.f;
+    for (int p = 0; p < parts; ++p) top = fmaxf(top, ml[p][0]);
+    v4f o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int p = 0; p < parts; ++p) {
+      const v2f x = load_device(from + (size_t)p * D), y = load_device(from + (size_t)p * D + 2);
+      const float f = exp2_fast(ml[p][0] - top);
+      sum += ml[p][1] * f;
+      o += (v4f){x[0], x[1], y[0], y[1]} * f;
+    }
+    const int i_new = (r0 + r) / a.g;
+    store_result<BF16>(a, (size_t)(s.first + i_new), h * a.g + (r0 + r) - i_new * a.g, c, o, sum, top);
+  }
+  if (tid == 0) *count = 0;
 }
 
 // Joins the splits of a row: a workgroup of four waves, a wave to a row, a lane to D / 64 channels.
@@ -353,7 +409,9 @@ __global__ void __launch_bounds__(256) combine_splits_kernel(PagedAttention a) {
   const int i = (int)(id % (unsigned)a.batch.max_new), b = (int)(id / (unsigned)a.batch.max_new);
   if (b >= a.batch.batch) return;
   const Sequence s = load_sequence(a.batch, b);
-  const int split_steps = a.plan.prompts && !(a.plan.few && s.n * a.g <= kFewRows) ? a.plan.prompt_split_steps : a.plan.split_steps;
+  const bool few = a.plan.few && (!a.plan.prompts || s.n * a.g <= kFewRows);
+  if (few && a.plan.few_joins) return;
+  const int split_steps = few ? a.plan.split_steps : a.plan.prompt_split_steps;
   int parts = ceil_div(ceil_div(s.len, kStep), split_steps);
   if (i >= s.n || parts <= 1) return;
   // the parts that hold a token which the row sees
@@ -423,13 +481,17 @@ hipError_t launch_paged_few(const PagedAttention& a, bool bf16, hipStream_t stre
 hipError_t launch_paged_combine(const PagedAttention& a, bool bf16, hipStream_t stream) { CQ_FOR_HEAD_DIM(launch_combine_d); }
 
 // Few rows: a workgroup per (sequence, KV head, tile of rows) and split.  Splits are of a fixed number of tokens, so that sequences of
-// different lengths have as many as they need; about kWorkgroups in all, a step for every wave at least.
+// different lengths have as many as they need: as many workgroups as are resident at once (two to a CU while their registers
+// allow it) if sequences are of the same length, a step for every wave at least.  Twice as many took 1 to 5 % longer at 64 x 8192, 8 x 65536
+// and 32 x 8192 tokens, 20 % at 8 x 4096 and 1 x 65536; 1.5 times as many up to 18 %.
+// While the partial results of a row of workgroups are few (4 KB of maxima and sums, 256 KB of values), the one that ends last joins them;
+// otherwise a launch of its own does, whose waves are many.
 // Many rows (over kFewRows per KV head): a workgroup takes a block of rows over a split; a CU holds one.  The
 // fewest splits that leave the last round of workgroups at least nine tenths full are taken, or those that fill it best: each costs its
 // partial results.  In a batch some sequences can have few rows all the same, whose workgroups are those of the other kernel.
 PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, int n_q_heads) {
-  constexpr long long kWorkgroups = 1024;
   PagedPlan p;
+  const long long cus = device_cu_count();
   const int g = n_q_heads / cache.heads;
   const long long rows = (long long)batch.max_new * g;
   const int steps = ceil_div(batch.len_bound, kStep);
@@ -440,17 +502,20 @@ PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, 
     p.row_tiles = few > 16 ? 2 : 1;
     p.row_blocks = (int)((few + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
     const long long beside = (long long)batch.batch * cache.heads * p.row_blocks;
-    long long want = kWorkgroups / beside;
-    const long long most = ceil_div(steps, 4);
+    long long want = cus * (cache.d * p.row_tiles <= 128 ? 2 : 1) / beside;
+    long long most = ceil_div(steps, 4);
+    if (most > kMostSplits) most = kMostSplits;
     if (want > most) want = most;
     if (want < 1) want = 1;
     p.split_steps = ceil_div(steps, (int)want);
     p.few_splits = p.splits = ceil_div(steps, p.split_steps);
+    const long long parts = few * p.few_splits;
+    p.few_joins = p.few_splits > 1 && parts <= 512 && parts * cache.d <= 65536;
   }
   if (p.prompts) {
     const int block = prompt_rows();
     p.prompt_blocks = (int)((rows + block - 1) / block);
-    const long long beside = (long long)batch.batch * cache.heads * p.prompt_blocks, cus = device_cu_count();
+    const long long beside = (long long)batch.batch * cache.heads * p.prompt_blocks;
     const long long most = steps / 8 < 32 ? steps / 8 : 32;
     int best = 1;
     double best_full = 0;
@@ -469,7 +534,8 @@ PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, 
   }
   if (p.splits > 1) {
     const size_t parts = (size_t)batch.n_tokens * n_q_heads * p.splits;
-    p.ws_acc_floats = (parts * 2 + 63) / 64 * 64;
+    if (p.few_joins) p.ws_ml_floats = ((size_t)batch.batch * cache.heads * p.row_blocks * 2 + 63) / 64 * 64;
+    p.ws_acc_floats = p.ws_ml_floats + (parts * 2 + 63) / 64 * 64;
     p.ws_bytes = ((p.ws_acc_floats + parts * cache.d) * sizeof(float) + 255) / 256 * 256;
     if (p.ws_bytes == 0) p.ws_bytes = 256;
   }

@@ -68,6 +68,7 @@ hipError_t launch_append(const PagedCacheArgs& cache, const PagedBatch& batch, b
 // How the attention of a step is spread: sequences of at most kFewRows (new token, query head) rows per KV head go to one kernel
 // (paged_few.hip), those of more to another (paged_prompt.hip).
 constexpr int kFewRows = 32;
+constexpr int kMostSplits = 128;   // below the 256 that a count holds
 struct PagedPlan {
   bool prompts = false;    // sequences of more rows are possible
   bool few = true;         // the first kernel runs
@@ -75,10 +76,11 @@ struct PagedPlan {
   int row_blocks = 1;      // its workgroups beside each other for the rows of a (sequence, KV head)
   int split_steps = 1;     // its steps of kStep tokens per split of a sequence
   int few_splits = 1;      // of the longest sequence
+  bool few_joins = false;  // it joins them itself
   int prompt_blocks = 1;   // the same of the second kernel
   int prompt_split_steps = 1, prompt_splits = 1;
   int splits = 1;          // the larger number of splits
-  size_t ws_acc_floats = 0;   // workspace: [m, l | acc], [rows][splits] each
+  size_t ws_ml_floats = 0, ws_acc_floats = 0;   // workspace: [counts | m, l | acc], the latter two [rows][splits]
   size_t ws_bytes = 256;
 };
 int prompt_rows();         // rows of a workgroup of the second kernel
@@ -93,6 +95,8 @@ struct PagedAttention {
   int causal;
   float scale_log2;        // softmax scale times log2(e)
   PagedPlan plan;
+  unsigned long long* counts;   // [batch][KV heads][row blocks] workgroups that have ended (decode_meet.h)
+  unsigned long long tag;       // of the call
   float* ml;               // [rows][splits][2] partial maxima and sums
   float* acc;              // [rows][splits][d]
 };

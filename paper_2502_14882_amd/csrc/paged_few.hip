@@ -89,38 +89,6 @@ __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAt
   int step1 = step0 + a.plan.split_steps;
   if (step1 > ceil_div(lim_hi, kStep)) step1 = ceil_div(lim_hi, kStep);
 
-  // queries: every row scaled by a power of two
-  v8h q[NT][T::kKeyOps];
-  float row_scale[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const uint16_t* p = static_cast<const uint16_t*>(a.q.data);
-    const bool there = r0 + 16 * t + n < rows;
-    if (there) p += at_row[t] * a.q.token_stride + at_head[t] * a.q.head_stride;
-    v4u raw[T::kKeyOps];
-    float most = 0.f;
-#pragma unroll
-    for (int j = 0; j < T::kKeyOps; ++j) {
-      const int c = j < 2 * T::kPieces ? (j / 2) * 64 + grp * 16 + (j % 2) * 8 : T::kPieces * 64 + grp * 8;
-      raw[j] = there ? *reinterpret_cast<const v4u*>(p + c) : (v4u){0, 0, 0, 0};
-      float x[8];
-      widen8<BF16>(raw[j], x);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) most = fmaxf(most, __builtin_isfinite(x[i]) ? fabsf(x[i]) : 0.f);
-    }
-    most = fmaxf(most, __shfl_xor(most, 16));
-    most = fmaxf(most, __shfl_xor(most, 32));
-    const float up = row_unit(most);
-    row_scale[t] = a.scale_log2 / up;
-#pragma unroll
-    for (int j = 0; j < T::kKeyOps; ++j) {
-      float x[8];
-      widen8<BF16>(raw[j], x);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) q[t][j][i] = (_Float16)(x[i] * up);
-    }
-  }
-
   const bool once = C.page <= 64 && a.plan.row_blocks == 1;
   const int32_t* table = a.batch.page_table + (size_t)b * a.batch.max_pages;
   auto place_of = [&](int step) {
@@ -131,6 +99,22 @@ __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAt
     w.offset = tok & (C.page - 1);
     return w;
   };
+  int step = step0 + wave;
+  Place here = {-1, 0}, next = {-1, 0};
+  if (step < step1) here = place_of(step);
+  // everything that the first step needs is asked for before the queries are made operands
+  v4u raw[NT][T::kKeyOps];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const uint16_t* p = static_cast<const uint16_t*>(a.q.data);
+    const bool there = r0 + 16 * t + n < rows;
+    if (there) p += at_row[t] * a.q.token_stride + at_head[t] * a.q.head_stride;
+#pragma unroll
+    for (int j = 0; j < T::kKeyOps; ++j) {
+      const int c = j < 2 * T::kPieces ? (j / 2) * 64 + grp * 16 + (j % 2) * 8 : T::kPieces * 64 + grp * 8;
+      raw[t][j] = there ? *reinterpret_cast<const v4u*>(p + c) : (v4u){0, 0, 0, 0};
+    }
+  }
   v4u key[4][T::kPieces > 0 ? T::kPieces : 1];
   v2u key_half[4];
   v4u val[T::kValueTiles];
@@ -166,6 +150,38 @@ __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAt
     next_val_scale = w.pid < 0 ? 0.f : C.v_scale[i];     // 0 marks tokens that are not there
   };
 
+  if (step < step1) {
+    load_scales(here);
+    load_keys(here);
+    load_values(here);
+    next = place_of(step + kWaves < step1 ? step + kWaves : step);
+  }
+  // queries: every row scaled by a power of two
+  v8h q[NT][T::kKeyOps];
+  float row_scale[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    float most = 0.f;
+#pragma unroll
+    for (int j = 0; j < T::kKeyOps; ++j) {
+      float x[8];
+      widen8<BF16>(raw[t][j], x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) most = fmaxf(most, __builtin_isfinite(x[i]) ? fabsf(x[i]) : 0.f);
+    }
+    most = fmaxf(most, __shfl_xor(most, 16));
+    most = fmaxf(most, __shfl_xor(most, 32));
+    const float up = row_unit(most);
+    row_scale[t] = a.scale_log2 / up;
+#pragma unroll
+    for (int j = 0; j < T::kKeyOps; ++j) {
+      float x[8];
+      widen8<BF16>(raw[t][j], x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) q[t][j][i] = (_Float16)(x[i] * up);
+    }
+  }
+
   v4f acc[NT][T::kValueTiles];
   float m[NT], l[NT];
 #pragma unroll
@@ -176,15 +192,6 @@ __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAt
     for (int c = 0; c < T::kValueTiles; ++c) acc[t][c] = (v4f){0.f, 0.f, 0.f, 0.f};
   }
 
-  int step = step0 + wave;
-  Place here = {-1, 0}, next = {-1, 0};
-  if (step < step1) {
-    here = place_of(step);
-    load_scales(here);
-    load_keys(here);
-    load_values(here);
-    next = place_of(step + kWaves < step1 ? step + kWaves : step);
-  }
   for (; step < step1; step += kWaves) {
     key_scale = next_key_scale;
     val_scale = next_val_scale;

@@ -64,6 +64,8 @@ int check_cache(const cqp_cache_t* c, bool pointers, cq::PagedCacheArgs* out) {
   int log2 = 4;
   while (log2 < 8 && (1 << log2) != c->page) ++log2;
   if ((1 << log2) != c->page) return fail(CQ_ERR_SHAPE, "page=%d is not 16, 32, 64, 128 or 256", c->page);
+  if ((double)c->n_kv_heads * c->page * c->head_dim >= 2147483648.0)
+    return fail(CQ_ERR_SHAPE, "a page of %d heads x %d tokens x %d channels is too large", c->n_kv_heads, c->page, c->head_dim);
   if ((double)c->n_pages * c->n_kv_heads * c->page * c->head_dim >= 4.0e18) return fail(CQ_ERR_SHAPE, "cache too large");
   if (pointers) {
     if (!c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale) return fail(CQ_ERR_NULL, "cache has a NULL pointer");

@@ -22,11 +22,14 @@ struct Sequence {
 };
 __device__ inline int clamp_int(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
 __device__ inline Sequence load_sequence(const PagedBatch& s, int b) {
+  // the same for all lanes (b is), and known to be to the compiler: branches on them are scalar
+  const int from = __builtin_amdgcn_readfirstlane(s.q_start[b]), to = __builtin_amdgcn_readfirstlane(s.q_start[b + 1]);
+  const int len = __builtin_amdgcn_readfirstlane(s.seq_lens[b]);
   Sequence q;
-  q.first = clamp_int(s.q_start[b], 0, s.n_tokens);
-  const int rows = clamp_int(s.q_start[b + 1], q.first, s.n_tokens) - q.first;
+  q.first = clamp_int(from, 0, s.n_tokens);
+  const int rows = clamp_int(to, q.first, s.n_tokens) - q.first;
   q.n = rows < s.max_new ? rows : s.max_new;
-  q.len = clamp_int(s.seq_lens[b], 0, s.len_bound);
+  q.len = clamp_int(len, 0, s.len_bound);
   q.pos0 = q.len - rows;
   return q;
 }
@@ -90,6 +93,9 @@ __device__ inline float row_unit(float most) {
   const int e = most > 0x1p-100f ? (int)(__builtin_bit_cast(unsigned, most) >> 23) - 127 - 14 : 0;
   return __builtin_bit_cast(float, (unsigned)(127 - e) << 23);
 }
+
+// 1 / x of a power of two between 2^-126 and 2^126
+__device__ inline float inverse_of_power(float x) { return __builtin_bit_cast(float, 0x7f000000u - __builtin_bit_cast(unsigned, x)); }
 
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 

@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAt
   __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
   __shared__ bool s_last;
   const PagedCacheArgs& C = a.cache;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n = lane & 15, grp = lane >> 4;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 15, grp = lane >> 4;
   unsigned id = blockIdx.x;
   const int split = (int)(id % (unsigned)a.plan.few_splits);
   id /= (unsigned)a.plan.few_splits;

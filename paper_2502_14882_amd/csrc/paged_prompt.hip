@@ -29,6 +29,7 @@ template <int D>
 struct Prompt {
   static constexpr int kKeyOps = D / 16;                              // operands of a tile of 32 keys
   static constexpr int kValueTiles = D / 32;
+  static constexpr int kAtOnce = D <= 128 ? kKeyOps : kKeyOps / 2;    // operands of keys in registers
   static constexpr int kPieces = (4 * D + kPromptThreads - 1) / kPromptThreads;   // of 16 codes, per thread, for keys as for values
   static constexpr bool kEven = 4 * D % kPromptThreads == 0;
   // bytes of an operand in LDS: padded such that the writes of eight neighbouring lanes fall into eight different banks' groups
@@ -54,7 +55,7 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_kernel(PagedAttention a
   uint8_t* const s_keys = s_tiles;
   uint8_t* const s_values = s_tiles + 2 * T::kKeyBytes;
   const PagedCacheArgs& C = a.cache;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n = lane & 31, half = lane >> 5;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 31, half = lane >> 5;
 
   // KV heads fastest: with eight of them a head's workgroups share an XCD and its L2; of the rows the last first, whose tokens are
   // the most where rows see up to their own
@@ -126,6 +127,10 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_kernel(PagedAttention a
     w->ks = w->pid < 0 ? 1.f : ks;
     w->vs = w->pid < 0 ? 0.f : vs;
   };
+  // a page's codes of this head: first + pid * stride, one multiplication (the host has checked that the stride fits 32 bits)
+  const unsigned page_bytes = (unsigned)(C.heads * C.page * D);
+  const uint8_t* const first_keys = C.k_codes + (((size_t)h << C.page_log2)) * D;
+  const uint8_t* const first_values = C.v_codes + (((size_t)h * D) << C.page_log2);
   v4u key[T::kPieces], val[T::kPieces];
   auto load_keys = [&](int step, int pid_of_lane) {
 #pragma unroll
@@ -133,19 +138,18 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_kernel(PagedAttention a
       const int p = tid + kPromptThreads * j, tok = p / T::kKeyOps, c = 16 * (p % T::kKeyOps);
       const int pid = __shfl(pid_of_lane, (tok >> 4) & 3);
       if (T::kEven || p < 4 * D) {
-        const int offset = (step * kStep + tok) & (C.page - 1);
-        key[j] = *reinterpret_cast<const v4u*>(C.k_codes + ((((size_t)(pid < 0 ? 0 : pid) * C.heads + h) << C.page_log2) + offset) * D + c);
+        const unsigned offset = (unsigned)((step * kStep + tok) & (C.page - 1)) * D + c;
+        key[j] = *reinterpret_cast<const v4u*>(first_keys + ((unsigned long long)(unsigned)(pid < 0 ? 0 : pid) * page_bytes + offset));
       }
     }
   };
   auto load_values = [&](int step, int pid) {
+    const unsigned offset = (unsigned)(step * kStep + 16 * (lane & 3)) & (unsigned)(C.page - 1);
+    const uint8_t* from = first_values + ((unsigned long long)(unsigned)(pid < 0 ? 0 : pid) * page_bytes + offset);
 #pragma unroll
     for (int j = 0; j < T::kPieces; ++j) {
       const int p = tid + kPromptThreads * j, c = p >> 2;
-      if (T::kEven || p < 4 * D) {
-        const int offset = (step * kStep + 16 * (lane & 3)) & (C.page - 1);
-        val[j] = *reinterpret_cast<const v4u*>(C.v_codes + ((((size_t)(pid < 0 ? 0 : pid) * C.heads + h) * D + c) << C.page_log2) + offset);
-      }
+      if (T::kEven || p < 4 * D) val[j] = *reinterpret_cast<const v4u*>(from + ((unsigned)c << C.page_log2));
     }
   };
   auto store_keys = [&](int buffer) {
@@ -163,7 +167,7 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_kernel(PagedAttention a
   // values in units of `unit`; where some row does not see some of the 64 tokens, those that nobody sees or that are not
   // there are cleared, and NaN codes of the others too: their tokens are noted, whose logits become NaN
   auto store_values = [&](int buffer, int step, const Groups& w, float unit) {
-    const float rel = w.vs == 0.f ? 1.f : w.vs / unit;
+    const float rel = w.vs == 0.f ? 1.f : w.vs * inverse_of_power(unit);
     const int tok = step * kStep + 16 * (lane & 3);
     const bool cut = step * kStep + kStep > block_lo || __any(w.pid < 0);
 #pragma unroll
@@ -193,13 +197,16 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_kernel(PagedAttention a
   // The unit of a step's values in LDS: the one so far while all of the step's scales lie within 2^-15 to 1 of it (codes times those are
   // exact in fp16), otherwise the largest of them.
   auto unit_of = [&](float unit, const Groups& w) {
-    float top = fmaxf(w.vs, __shfl_xor(w.vs, 1));
-    top = fmaxf(top, __shfl_xor(top, 2));
-    float low = w.vs == 0.f ? top : w.vs;
-    low = fminf(low, __shfl_xor(low, 1));
-    low = fminf(low, __shfl_xor(low, 2));
-    const float next = top > unit || low < unit * 0x1p-15f ? top : unit;
-    return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, top == 0.f ? unit : next)));
+    unsigned top = 0, low = 0xffffffffu;                              // positive floats compare as their bits
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned x = (unsigned)__builtin_amdgcn_readlane(__builtin_bit_cast(int, w.vs), i);
+      top = x > top ? x : top;
+      low = x - 1 < low ? x - 1 : low;                                // groups that are not there, 0, come last
+    }
+    if (top == 0) return unit;
+    const float most = __builtin_bit_cast(float, top), least = __builtin_bit_cast(float, low + 1);
+    return most > unit || least < unit * 0x1p-15f ? most : unit;
   };
 
   v16f acc[T::kValueTiles];
@@ -211,13 +218,29 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_kernel(PagedAttention a
 
   // The 32 tokens 32 t .. of a step.
   auto attend = [&](int buffer, int step, int t, const Groups& w) {
+    // operands are read from LDS well before their products: those of the keys at once (in halves from 160 channels on), those
+    // of the values before the softmax
     const uint8_t* keys = s_keys + buffer * T::kKeyBytes + t * T::kKeyOps * T::kKeyStride + lane * 16;
+    const uint8_t* values = s_values + buffer * T::kValueBytes + 2 * t * T::kValueStride + lane * 16;
     v16f sc;
 #pragma unroll
     for (int e = 0; e < 16; ++e) sc[e] = 0.f;
 #pragma unroll
-    for (int j = 0; j < T::kKeyOps; ++j)
-      sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const v8h*>(keys + j * T::kKeyStride), q[j], sc, 0, 0, 0);
+    for (int j0 = 0; j0 < T::kKeyOps; j0 += T::kAtOnce) {
+      v8h k[T::kAtOnce];
+#pragma unroll
+      for (int j = 0; j < T::kAtOnce; ++j) k[j] = *reinterpret_cast<const v8h*>(keys + (j0 + j) * T::kKeyStride);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < T::kAtOnce; ++j) sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[j], q[j0 + j], sc, 0, 0, 0);
+    }
+    v8h v[2][T::kValueTiles];
+    constexpr int kEarly = D <= 128 ? 2 : 1;
+#pragma unroll
+    for (int i = 0; i < kEarly; ++i)
+#pragma unroll
+      for (int c = 0; c < T::kValueTiles; ++c) v[i][c] = *reinterpret_cast<const v8h*>(values + (c * 4 + i) * T::kValueStride);
+    __builtin_amdgcn_sched_barrier(0);
     if (step * kStep + kStep > block_lo || __any(w.pid < 0)) {        // where store_values looks for NaN codes
       const unsigned long long there = __ballot(w.pid >= 0) >> (2 * t);      // bit i: group i
       const unsigned nan = s_nan[step % 3][t];
@@ -262,13 +285,14 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_kernel(PagedAttention a
         p[i][e] = two[0];
         p[i][e + 1] = two[1];
       }
-    const uint8_t* values = s_values + buffer * T::kValueBytes + 2 * t * T::kValueStride + lane * 16;
+#pragma unroll
+    for (int i = kEarly; i < 2; ++i)
+#pragma unroll
+      for (int c = 0; c < T::kValueTiles; ++c) v[i][c] = *reinterpret_cast<const v8h*>(values + (c * 4 + i) * T::kValueStride);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int c = 0; c < T::kValueTiles; ++c)
-        acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const v8h*>(values + (c * 4 + i) * T::kValueStride), p[i],
-                                                        acc[c], 0, 0, 0);
+      for (int c = 0; c < T::kValueTiles; ++c) acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[i][c], p[i], acc[c], 0, 0, 0);
   };
 
   if (steps > 0) {
@@ -306,7 +330,7 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_kernel(PagedAttention a
       pid = page_of(at(i + 3));
       if (at(i) * kStep < wave_hi) {
         if (unit != acc_unit) {
-          const float f = acc_unit / unit;
+          const float f = acc_unit * inverse_of_power(unit);
 #pragma unroll
           for (int c = 0; c < T::kValueTiles; ++c) acc[c] *= f;
           acc_unit = unit;

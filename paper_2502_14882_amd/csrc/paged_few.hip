@@ -520,7 +520,7 @@ PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, 
     p.few_joins = p.few_splits > 1 && parts <= 512 && parts * cache.d <= 65536;
   }
   if (p.prompts) {
-    const int block = prompt_rows();
+    const int block = prompt_rows(cache.d);
     p.prompt_blocks = (int)((rows + block - 1) / block);
     const long long beside = (long long)batch.batch * cache.heads * p.prompt_blocks;
     const long long most = steps / 8 < 32 ? steps / 8 : 32;

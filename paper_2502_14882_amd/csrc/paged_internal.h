@@ -83,7 +83,7 @@ struct PagedPlan {
   size_t ws_ml_floats = 0, ws_acc_floats = 0;   // workspace: [counts | m, l | acc], the latter two [rows][splits]
   size_t ws_bytes = 256;
 };
-int prompt_rows();         // rows of a workgroup of the second kernel
+int prompt_rows(int d);    // rows of a workgroup of the second kernel
 PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, int n_q_heads);
 
 struct PagedAttention {

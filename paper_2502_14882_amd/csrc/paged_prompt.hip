@@ -21,22 +21,19 @@
 namespace cq {
 namespace {
 
-constexpr int kPromptWaves = 8;
-constexpr int kPromptThreads = 64 * kPromptWaves;
-constexpr int kPromptRows = 32 * kPromptWaves;
-
 template <int D>
 struct Prompt {
-  static constexpr int kKeyOps = D / 16;                              // operands of a tile of 32 keys
+  static constexpr int kWaves = D <= 160 ? 8 : 4;                     // two to a SIMD while 256 registers hold what one needs
+  static constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves;
+  static constexpr int kOps = D / 16;                                 // operands of 32 keys, and of 32 tokens' values
   static constexpr int kValueTiles = D / 32;
-  static constexpr int kAtOnce = D <= 128 ? kKeyOps : kKeyOps / 2;    // operands of keys in registers
-  static constexpr int kPieces = (4 * D + kPromptThreads - 1) / kPromptThreads;   // of 16 codes, per thread, for keys as for values
-  static constexpr bool kEven = 4 * D % kPromptThreads == 0;
+  static constexpr int kPieces = (4 * D + kThreads - 1) / kThreads;   // of 16 codes, per thread, for keys as for values
+  static constexpr bool kEven = 4 * D % kThreads == 0;
   // bytes of an operand in LDS: padded such that the writes of eight neighbouring lanes fall into eight different banks' groups
   static constexpr int kKeyStride = 1024 + 16, kValueStride = 1024 + 32;
-  static constexpr int kKeyBytes = 2 * kKeyOps * kKeyStride, kValueBytes = 4 * kValueTiles * kValueStride;
+  static constexpr int kKeyBytes = 2 * kOps * kKeyStride, kValueBytes = 2 * kOps * kValueStride;
   static constexpr int kOutStride = D + 8;                            // fp16 elements between the rows of the result in LDS
-  static constexpr int kOutBytes = kPromptRows * kOutStride * 2;
+  static constexpr int kOutBytes = kRows * kOutStride * 2;
   static constexpr int kTileBytes = 2 * (kKeyBytes + kValueBytes);
   static constexpr int kLds = kTileBytes > kOutBytes ? kTileBytes : kOutBytes;
 };
@@ -48,7 +45,7 @@ struct Groups {
 };
 
 template <int D, bool BF16>
-__global__ void __launch_bounds__(kPromptThreads) prompt_kernel(PagedAttention a) {
+__global__ void __launch_bounds__(Prompt<D>::kThreads) prompt_kernel(PagedAttention a) {
   using T = Prompt<D>;
   extern __shared__ __align__(16) uint8_t s_tiles[];                  // [2][keys], [2][values]
   __shared__ unsigned s_nan[3][2];
@@ -67,17 +64,15 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_kernel(PagedAttention a
   const int split = (int)(id % (unsigned)a.plan.prompt_splits);
   const int rb = a.plan.prompt_blocks - 1 - (int)(id / (unsigned)a.plan.prompt_splits);
   const Sequence s = load_sequence(a.batch, b);
-  const int rows = s.n * a.g, block0 = rb * kPromptRows;
+  const int rows = s.n * a.g, block0 = rb * T::kRows;
   if (block0 >= rows || (a.plan.few && rows <= kFewRows)) return;
   const int parts = ceil_div(ceil_div(s.len, kStep), a.plan.prompt_split_steps);
   if (split >= (parts > 1 ? parts : 1)) return;
 
   auto sees = [&](int r) { return a.causal ? clamp_int(s.pos0 + r / a.g + 1, 0, s.len) : s.len; };
-  const int block_last = (block0 + kPromptRows < rows ? block0 + kPromptRows : rows) - 1;
+  const int block_last = (block0 + T::kRows < rows ? block0 + T::kRows : rows) - 1;
   const int block_lo = sees(block0), block_hi = sees(block_last);
   const int r0 = block0 + 32 * wave;                                   // this wave's rows
-  const int wave_last = (r0 + 32 < rows ? r0 + 32 : rows) - 1;
-  const int wave_hi = r0 < rows ? sees(wave_last) : 0;
   const int step0 = split * a.plan.prompt_split_steps;
   int step1 = step0 + a.plan.prompt_split_steps;
   if (step1 > ceil_div(block_hi, kStep)) step1 = ceil_div(block_hi, kStep);
@@ -87,15 +82,15 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_kernel(PagedAttention a
   const bool row_there = row < rows;
   const long long row_token = s.first + row_new;
   const int row_head = h * a.g + row - row_new * a.g, limit = row_there ? sees(row) : 0;
-  v8h q[T::kKeyOps];
+  v8h q[T::kOps];
   float row_scale;
   {
     const uint16_t* p = static_cast<const uint16_t*>(a.q.data);
     if (row_there) p += row_token * a.q.token_stride + row_head * a.q.head_stride;
-    v4u raw[T::kKeyOps];
+    v4u raw[T::kOps];
     float most = 0.f;
 #pragma unroll
-    for (int j = 0; j < T::kKeyOps; ++j) {
+    for (int j = 0; j < T::kOps; ++j) {
       raw[j] = row_there ? *reinterpret_cast<const v4u*>(p + 16 * j + 8 * half) : (v4u){0, 0, 0, 0};
       float x[8];
       widen8<BF16>(raw[j], x);
@@ -106,7 +101,7 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_kernel(PagedAttention a
     const float up = row_unit(most);
     row_scale = a.scale_log2 / up;
 #pragma unroll
-    for (int j = 0; j < T::kKeyOps; ++j) {
+    for (int j = 0; j < T::kOps; ++j) {
       float x[8];
       widen8<BF16>(raw[j], x);
 #pragma unroll
@@ -135,7 +130,7 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_kernel(PagedAttention a
   auto load_keys = [&](int step, int pid_of_lane) {
 #pragma unroll
     for (int j = 0; j < T::kPieces; ++j) {
-      const int p = tid + kPromptThreads * j, tok = p / T::kKeyOps, c = 16 * (p % T::kKeyOps);
+      const int p = tid + T::kThreads * j, tok = p / T::kOps, c = 16 * (p % T::kOps);
       const int pid = __shfl(pid_of_lane, (tok >> 4) & 3);
       if (T::kEven || p < 4 * D) {
         const unsigned offset = (unsigned)((step * kStep + tok) & (C.page - 1)) * D + c;
@@ -148,17 +143,17 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_kernel(PagedAttention a
     const uint8_t* from = first_values + ((unsigned long long)(unsigned)(pid < 0 ? 0 : pid) * page_bytes + offset);
 #pragma unroll
     for (int j = 0; j < T::kPieces; ++j) {
-      const int p = tid + kPromptThreads * j, c = p >> 2;
+      const int p = tid + T::kThreads * j, c = p >> 2;
       if (T::kEven || p < 4 * D) val[j] = *reinterpret_cast<const v4u*>(from + ((unsigned)c << C.page_log2));
     }
   };
   auto store_keys = [&](int buffer) {
 #pragma unroll
     for (int j = 0; j < T::kPieces; ++j) {
-      const int p = tid + kPromptThreads * j, tok = p / T::kKeyOps, op = p % T::kKeyOps;
+      const int p = tid + T::kThreads * j, tok = p / T::kOps, op = p % T::kOps;
       if (T::kEven || p < 4 * D) {
         const int t = tok & 31, m = (t & 0x13) | (t & 4) << 1 | (t & 8) >> 1;
-        uint8_t* to = s_keys + buffer * T::kKeyBytes + ((tok >> 5) * T::kKeyOps + op) * T::kKeyStride + m * 16;
+        uint8_t* to = s_keys + buffer * T::kKeyBytes + ((tok >> 5) * T::kOps + op) * T::kKeyStride + m * 16;
         *reinterpret_cast<v8h*>(to) = codes_to_half(key[j][0], key[j][1], 1.f);
         *reinterpret_cast<v8h*>(to + 512) = codes_to_half(key[j][2], key[j][3], 1.f);
       }
@@ -172,7 +167,7 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_kernel(PagedAttention a
     const bool cut = step * kStep + kStep > block_lo || __any(w.pid < 0);
 #pragma unroll
     for (int j = 0; j < T::kPieces; ++j) {
-      const int p = tid + kPromptThreads * j, c = p >> 2;
+      const int p = tid + T::kThreads * j, c = p >> 2;
       if (T::kEven || p < 4 * D) {
         v4u x = val[j];
         if (cut) {
@@ -216,30 +211,23 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_kernel(PagedAttention a
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[c][e] = 0.f;
 
-  // The 32 tokens 32 t .. of a step.
-  auto attend = [&](int buffer, int step, int t, const Groups& w) {
-    // operands are read from LDS well before their products: those of the keys at once (in halves from 160 channels on), those
-    // of the values before the softmax
-    const uint8_t* keys = s_keys + buffer * T::kKeyBytes + t * T::kKeyOps * T::kKeyStride + lane * 16;
-    const uint8_t* values = s_values + buffer * T::kValueBytes + 2 * t * T::kValueStride + lane * 16;
-    v16f sc;
+  // Half h of the sequence of halves of steps (32 tokens each).  Three things that do not depend on each other, dealt out in
+  // kOps groups such that the matrix cores work under the softmax: the logits of half h + 1 (`next`), the weights of half h (from `now`, to
+  // `p`), and the products of half h - 1's weights (`before`) with its values.
+  auto half_step = [&](const uint8_t* keys, const uint8_t* values, int step, int t, const Groups& w, v16f& now, v16f& next, v8h (&p)[2],
+                       v8h (&before)[2]) {
+    auto key_op = [&](int j) { return *reinterpret_cast<const v8h*>(keys + j * T::kKeyStride); };
+    // in the order [16 tokens][32 channels]; in LDS the four operands of 32 channels lie together
+    auto value_op = [&](int j) {
+      return *reinterpret_cast<const v8h*>(values + (j % T::kValueTiles * 4 + j / T::kValueTiles) * T::kValueStride);
+    };
+    constexpr int kAhead = 2;
+    v8h k[kAhead + 1], v[kAhead + 1];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) sc[e] = 0.f;
-#pragma unroll
-    for (int j0 = 0; j0 < T::kKeyOps; j0 += T::kAtOnce) {
-      v8h k[T::kAtOnce];
-#pragma unroll
-      for (int j = 0; j < T::kAtOnce; ++j) k[j] = *reinterpret_cast<const v8h*>(keys + (j0 + j) * T::kKeyStride);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int j = 0; j < T::kAtOnce; ++j) sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[j], q[j0 + j], sc, 0, 0, 0);
+    for (int j = 0; j < kAhead; ++j) {
+      k[j] = key_op(j);
+      v[j] = value_op(j);
     }
-    v8h v[2][T::kValueTiles];
-    constexpr int kEarly = D <= 128 ? 2 : 1;
-#pragma unroll
-    for (int i = 0; i < kEarly; ++i)
-#pragma unroll
-      for (int c = 0; c < T::kValueTiles; ++c) v[i][c] = *reinterpret_cast<const v8h*>(values + (c * 4 + i) * T::kValueStride);
     __builtin_amdgcn_sched_barrier(0);
     if (step * kStep + kStep > block_lo || __any(w.pid < 0)) {        // where store_values looks for NaN codes
       const unsigned long long there = __ballot(w.pid >= 0) >> (2 * t);      // bit i: group i
@@ -251,97 +239,134 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_kernel(PagedAttention a
         const int live = there >> i & 1 ? limit - step * kStep - 32 * t - first : 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float x = sc[8 * i + e];
-          sc[8 * i + e] = e < live ? (bad >> e & 1 ? __builtin_nanf("") : x) : -__builtin_inff();
+          const float x = now[8 * i + e];
+          now[8 * i + e] = e < live ? (bad >> e & 1 ? __builtin_nanf("") : x) : -__builtin_inff();
         }
+        __builtin_amdgcn_sched_barrier(0);                            // (all comparisons at once would not fit the scalar registers)
       }
     }
     float f[2], top = kNoMax;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       f[i] = row_scale * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w.ks), 2 * t + i));
-      float best = sc[8 * i];
+      float best = now[8 * i];
 #pragma unroll
-      for (int e = 1; e < 8; ++e) best = fmaxf(best, sc[8 * i + e]);
+      for (int e = 1; e < 8; ++e) best = fmaxf(best, now[8 * i + e]);
       top = fmaxf(top, best * f[i]);
     }
     if (__any(top > m + 8.f)) {
+      // the weights before are relative to the old reference: their products are added first
+#pragma unroll
+      for (int j = 0; j < T::kOps; ++j) {
+        acc[j % T::kValueTiles] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value_op(j), before[j / T::kValueTiles], acc[j % T::kValueTiles], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) before[i] = (v8h){0, 0, 0, 0, 0, 0, 0, 0};
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float now = fmaxf(m, top), g = exp2_fast(m - now);
-      m = now;
+      const float to = fmaxf(m, top), g = exp2_fast(m - to);
+      m = to;
       l *= g;
 #pragma unroll
       for (int c = 0; c < T::kValueTiles; ++c) acc[c] *= g;
     }
-    v8h p[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int e = 0; e < 16; ++e) next[e] = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        const float x = exp2_fast(__builtin_fmaf(sc[8 * i + e], f[i], -m));
-        const float y = exp2_fast(__builtin_fmaf(sc[8 * i + e + 1], f[i], -m));
-        const v2h two = {(_Float16)x, (_Float16)y};
-        l = __builtin_amdgcn_fdot2(two, (v2h){(_Float16)1.f, (_Float16)1.f}, l, false);
-        p[i][e] = two[0];
-        p[i][e + 1] = two[1];
+    for (int j = 0; j < T::kOps; ++j) {
+      if (j + kAhead < T::kOps) {
+        k[(j + kAhead) % (kAhead + 1)] = key_op(j + kAhead);
+        v[(j + kAhead) % (kAhead + 1)] = value_op(j + kAhead);
       }
+      if (j == 0) __builtin_amdgcn_s_setprio(1);
+      next = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[j % (kAhead + 1)], q[j], next, 0, 0, 0);
+      acc[j % T::kValueTiles] =
+          __builtin_amdgcn_mfma_f32_32x32x16_f16(v[j % (kAhead + 1)], before[j / T::kValueTiles], acc[j % T::kValueTiles], 0, 0, 0);
 #pragma unroll
-    for (int i = kEarly; i < 2; ++i)
-#pragma unroll
-      for (int c = 0; c < T::kValueTiles; ++c) v[i][c] = *reinterpret_cast<const v8h*>(values + (c * 4 + i) * T::kValueStride);
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int c = 0; c < T::kValueTiles; ++c) acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[i][c], p[i], acc[c], 0, 0, 0);
+      for (int pair = 8 * j / T::kOps; pair < 8 * (j + 1) / T::kOps; ++pair) {
+        const int i = pair >> 2, e = 2 * pair;
+        const float x = exp2_fast(__builtin_fmaf(now[e], f[i], -m)), y = exp2_fast(__builtin_fmaf(now[e + 1], f[i], -m));
+        v2h two = {(_Float16)x, (_Float16)y};
+        asm volatile("" : "+v"(two));        // here, and not where the next half uses it
+        l = __builtin_amdgcn_fdot2(two, (v2h){(_Float16)1.f, (_Float16)1.f}, l, false);
+        p[i][e & 7] = two[0];
+        p[i][(e & 7) + 1] = two[1];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_s_setprio(0);
   };
 
   if (steps > 0) {
-    // Step i: its products; written to LDS: i + 1; asked for: i + 2.  Beyond the last step the last one's codes are loaded again, and not
-    // used.
+    // Step i: its halves 2 i and 2 i + 1; logits of 2 i + 1 and 2 i + 2, values of 2 i - 1 and 2 i.  Behind the barrier between the two nobody reads
+    // the keys of i and the values of i - 1 any more: keys of i + 2 and values of i + 1 take their places; asked for: keys of
+    // i + 3, values of i + 2.  Beyond the last step the last one's codes are loaded again, and not used.
     auto at = [&](int i) { return step0 + (i < steps ? i : steps - 1); };
-    Groups g0, g1;
+    auto keys_of = [&](int i, int t) { return s_keys + (i & 1) * T::kKeyBytes + t * T::kOps * T::kKeyStride + lane * 16; };
+    auto values_of = [&](int i, int t) { return s_values + (i & 1) * T::kValueBytes + 2 * t * T::kValueStride + lane * 16; };
+    Groups g0, g1, g2;
     if (tid < 6) s_nan[tid >> 1][tid & 1] = 0;
+    // the values "before" the first half are multiplied by 0
+    for (int i = tid; i < T::kValueBytes / 16; i += T::kThreads)
+      *reinterpret_cast<v4u*>(s_values + T::kValueBytes + 16 * i) = (v4u){0, 0, 0, 0};
     g0.pid = page_of(at(0));
     g1.pid = page_of(at(1));
+    g2.pid = page_of(at(2));
     load_scales(&g0);
+    load_scales(&g1);
     load_keys(at(0), g0.pid);
     load_values(at(0), g0.pid);
-    __syncthreads();                                                  // s_nan
-    float unit = unit_of(1.f, g0), next_unit = unit;
     store_keys(0);
-    store_values(0, at(0), g0, unit);
-    load_scales(&g1);
     load_keys(at(1), g1.pid);
+    __syncthreads();                                                  // s_nan
+    float unit = unit_of(1.f, g0);
+    store_values(0, at(0), g0, unit);
     load_values(at(1), g1.pid);
-    int pid = page_of(at(2));
+    store_keys(1);
+    load_keys(at(2), g2.pid);
+    int pid = page_of(at(3));
+    __syncthreads();
+    v16f sc0, sc1;
+    v8h p0[2], p1[2];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sc0[e] = 0.f;
+#pragma unroll
+    for (int j = 0; j < T::kOps; ++j)
+      sc0 = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const v8h*>(keys_of(0, 0) + j * T::kKeyStride), q[j], sc0, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) p1[i] = (v8h){0, 0, 0, 0, 0, 0, 0, 0};
+    acc_unit = unit;
     for (int i = 0; i < steps; ++i) {
+      if (at(i) * kStep + kStep > block_lo || __any(g0.pid < 0)) __syncthreads();        // s_nan of this step
+      half_step(keys_of(i, 1), values_of(i + 1, 1), at(i), 0, g0, sc0, sc1, p0, p1);     // values_of(i - 1, 1): the same buffer
       __syncthreads();
       if (tid < 2) s_nan[(step0 + i + 2) % 3][tid] = 0;               // last read a step ago
-      if (i + 1 < steps) {
-        next_unit = unit_of(unit, g1);
-        store_keys((i + 1) & 1);
-        store_values((i + 1) & 1, at(i + 1), g1, next_unit);
-      }
-      Groups g2;
-      g2.pid = pid;
-      load_scales(&g2);
-      load_keys(at(i + 2), pid);
-      load_values(at(i + 2), pid);
-      pid = page_of(at(i + 3));
-      if (at(i) * kStep < wave_hi) {
-        if (unit != acc_unit) {
-          const float f = acc_unit * inverse_of_power(unit);
+      if (unit != acc_unit) {
+        const float f = acc_unit * inverse_of_power(unit);
 #pragma unroll
-          for (int c = 0; c < T::kValueTiles; ++c) acc[c] *= f;
-          acc_unit = unit;
-        }
-        attend(i & 1, at(i), 0, g0);
-        attend(i & 1, at(i), 1, g0);
+        for (int c = 0; c < T::kValueTiles; ++c) acc[c] *= f;
+        acc_unit = unit;
       }
-      unit = next_unit;
+      if (i + 1 < steps) {
+        unit = unit_of(unit, g1);
+        store_values((i + 1) & 1, at(i + 1), g1, unit);
+        if (i + 2 < steps) store_keys(i & 1);
+      }
+      load_scales(&g2);
+      load_values(at(i + 2), g2.pid);
+      load_keys(at(i + 3), pid);
+      half_step(keys_of(i + 1, 0), values_of(i, 0), at(i), 1, g0, sc1, sc0, p1, p0);
       g0 = g1;
       g1 = g2;
+      g2.pid = pid;
+      pid = page_of(at(i + 4));
     }
+    const uint8_t* values = values_of(steps - 1, 1);
+#pragma unroll
+    for (int j = 0; j < T::kOps; ++j)
+      acc[j % T::kValueTiles] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+          *reinterpret_cast<const v8h*>(values + (j % T::kValueTiles * 4 + j / T::kValueTiles) * T::kValueStride), p1[j / T::kValueTiles],
+          acc[j % T::kValueTiles], 0, 0, 0);
   }
 
   // ---- results
@@ -389,13 +414,13 @@ hipError_t launch_prompt_d(const PagedAttention& a, bool bf16, hipStream_t strea
   static std::atomic<size_t> raised[2][kPagedDevices];
   const hipError_t e = raise_lds(reinterpret_cast<const void*>(kernel), Prompt<D>::kLds, raised[bf16]);
   if (e != hipSuccess) return e;
-  kernel<<<dim3((unsigned)blocks), dim3(kPromptThreads), Prompt<D>::kLds, stream>>>(a);
+  kernel<<<dim3((unsigned)blocks), dim3(Prompt<D>::kThreads), Prompt<D>::kLds, stream>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-int prompt_rows() { return kPromptRows; }
+int prompt_rows(int d) { return d <= 160 ? Prompt<160>::kRows : Prompt<192>::kRows; }
 
 hipError_t launch_paged_prompt(const PagedAttention& a, bool bf16, hipStream_t stream) { CQ_FOR_HEAD_DIM(launch_prompt_d); }
 

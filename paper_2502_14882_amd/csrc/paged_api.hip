@@ -118,6 +118,7 @@ int check_rope(const cqp_rope_t* r, const int32_t* positions, int n_tokens, int 
   out->inv_freq = r->inv_freq;
   out->positions = positions;
   out->half = r->rot_dim / 2;
+  out->n_axes = r->n_axes;
   out->adjacent = r->pairs == CQP_PAIRS_ADJACENT;
   out->sign = 1.0f;
   return CQ_OK;

@@ -63,12 +63,21 @@ __device__ inline void unit_channels(const RopeArgs& rope, int u, int* c0, int* 
 }
 __device__ inline bool unit_turns(const RopeArgs& rope, int u) { return 8 * u < rope.half; }
 
+typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
+
 __device__ inline void unit_angles(const RopeArgs& rope, int n_tokens, int token, int u, CosSin* cs) {
+  const unsigned long long axes = *reinterpret_cast<const unsigned long long*>(rope.axis_of + 8 * u);
+  const v4f_any* freq = reinterpret_cast<const v4f_any*>(rope.inv_freq + 8 * u);
+  const v4f f0 = freq[0], f1 = freq[1];
+  // the token's place on every axis
+  const int32_t* at = rope.positions + token;
+  const int p0 = at[0], p1 = rope.n_axes > 1 ? at[n_tokens] : 0;
+  const int p2 = rope.n_axes > 2 ? at[2 * (size_t)n_tokens] : 0, p3 = rope.n_axes > 3 ? at[3 * (size_t)n_tokens] : 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int pair = 8 * u + i;
-    const int pos = rope.positions[(size_t)rope.axis_of[pair] * n_tokens + token];
-    cos_sin((double)pos * (double)rope.inv_freq[pair], &cs->c[i], &cs->s[i]);
+    const int axis = (int)(axes >> (8 * i)) & 3;
+    const int pos = axis & 2 ? (axis & 1 ? p3 : p2) : (axis & 1 ? p1 : p0);
+    cos_sin((double)pos * (double)(i < 4 ? f0[i & 3] : f1[i & 3]), &cs->c[i], &cs->s[i]);
     cs->s[i] *= rope.sign;
   }
 }
@@ -92,13 +101,10 @@ __device__ inline void turn_unit(const RopeArgs& rope, const CosSin& cs, float* 
   }
 }
 
-template <bool BF16>
-__device__ inline void load_unit(const HeadRows& t, long long token, int head, int c0, int c1, float* x) {
-  const uint16_t* p = static_cast<const uint16_t*>(t.data) + token * t.token_stride + head * t.head_stride;
-  const v4u a = *reinterpret_cast<const v4u*>(p + c0), b = *reinterpret_cast<const v4u*>(p + c1);
-  widen8<BF16>(a, x);
-  widen8<BF16>(b, x + 8);
+__device__ inline const uint16_t* row_of(const HeadRows& t, long long token, int head) {
+  return static_cast<const uint16_t*>(t.data) + token * t.token_stride + head * t.head_stride;
 }
+__device__ inline v4u load8(const uint16_t* p) { return *reinterpret_cast<const v4u*>(p); }
 
 // Thread -> (token, group of heads, unit), units fastest.  The heads of two tensors are counted through.
 struct RotateWork {
@@ -124,7 +130,10 @@ __device__ inline void rotate_thread(const RopeArgs& rope, const RotateWork& w, 
   for (int h = h0; h < h1; ++h) {
     const int t = h >= w.in[0].heads, head = t ? h - w.in[0].heads : h;
     float x[16];
-    load_unit<BF16>(w.in[t], token, head, c0, c1, x);
+    const uint16_t* from = row_of(w.in[t], token, head);
+    const v4u lo = load8(from + c0), hi = load8(from + c1);
+    widen8<BF16>(lo, x);
+    widen8<BF16>(hi, x + 8);
     if (turns) turn_unit(rope, cs, x);
     uint16_t* p = static_cast<uint16_t*>(w.out[t].data) + token * w.out[t].token_stride + head * w.out[t].head_stride;
     *reinterpret_cast<v4u*>(p + c0) = narrow8<BF16>(x);
@@ -158,7 +167,9 @@ RotateWork plan_rotate(int n_tokens, int d, const HeadRows* in, const HeadRows* 
 long long rotate_threads(const RotateWork& w) { return (long long)w.n_tokens * w.units * w.groups; }
 
 // ---- append
-constexpr int kItems = 4;          // units that a thread holds
+constexpr int kSlots = 4;          // pieces of 16 elements of the keys that a thread holds, half as many of 32 of the values
+constexpr int kMostThreads = 1024;
+constexpr long long kQueriesApart = 1 << 23;   // elements
 constexpr float kMinScale = 0x1p-100f;
 
 // The smallest power of two s >= 2^-100 with m <= 448 s: 448 = 1.75 * 2^8, so the exponent rises where the
@@ -170,22 +181,38 @@ __device__ inline float scale_for(float m) {
 }
 
 struct AppendArgs {
+  RopeArgs rope;
   PagedCacheArgs cache;
   PagedBatch batch;
   HeadRows k, v;
-  RopeArgs rope;
   RotateWork q;
   int tasks;               // pages that a sequence's new tokens can reach
+  int heads_per_block, groups;
   unsigned page_blocks;    // workgroups for pages; those behind turn queries
 };
 
+__device__ inline float magnitude(float x) { return __builtin_isfinite(x) ? fabsf(x) : 0.f; }
 // x / scale for codes: NaN for what is not finite
 __device__ inline float coded(float x, float inv) { return __builtin_isfinite(x) ? x * inv : __builtin_nanf(""); }
 
+// The largest of a wave's magnitudes into `most` (bits of floats >= 0 compare as they do); `spread`: lanes hold values of different heads.
+__device__ inline void fold_most(unsigned* most, float x, bool spread) {
+  if (spread) {
+    atomicMax(most, __builtin_bit_cast(unsigned, x));
+    return;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
+  if ((threadIdx.x & 63) == 0) atomicMax(most, __builtin_bit_cast(unsigned, x));
+}
+
+// One page of a sequence, heads_per_block heads of the keys or of the values.
+//   keys:   thread -> (token, 16 channels that hold whole pairs), a slot per head: the angles serve all of them
+//   values: thread -> (head, 4 tokens, 8 channels): a channel's four codes are one word, which turn in LDS
 template <bool BF16>
-__global__ void __launch_bounds__(1024) append_kernel(AppendArgs a) {
-  extern __shared__ __align__(16) uint8_t s_turn[];          // values: [d][page + 4]
-  __shared__ float s_most[16];
+__global__ void __launch_bounds__(kMostThreads) append_kernel(AppendArgs a) {
+  extern __shared__ __align__(16) uint8_t s_turn[];          // values: [heads][d][page + 4]
+  __shared__ unsigned s_most[kSlots];
   const int tid = threadIdx.x, threads = blockDim.x;
   unsigned id = blockIdx.x;
   if (id >= a.page_blocks) {
@@ -195,8 +222,9 @@ __global__ void __launch_bounds__(1024) append_kernel(AppendArgs a) {
   const PagedCacheArgs& C = a.cache;
   const bool value = id & 1;
   id >>= 1;
-  const int h = (int)(id % (unsigned)C.heads);
-  id /= (unsigned)C.heads;
+  const int h0 = (int)(id % (unsigned)a.groups) * a.heads_per_block;
+  const int heads = C.heads - h0 < a.heads_per_block ? C.heads - h0 : a.heads_per_block;
+  id /= (unsigned)a.groups;
   const int task = (int)(id % (unsigned)a.tasks), b = (int)(id / (unsigned)a.tasks);
   const Sequence s = load_sequence(a.batch, b);
   if (s.n == 0) return;
@@ -207,102 +235,175 @@ __global__ void __launch_bounds__(1024) append_kernel(AppendArgs a) {
   const int pid = a.batch.page_table[(size_t)b * a.batch.max_pages + index];      // place < to <= len: within the row
   if ((unsigned)pid >= (unsigned)C.n_pages) return;
   const int s0 = from > place ? from - place : 0, s1 = to - place < C.page ? to - place : C.page;
-  const int live = s1 - s0, units = C.d / 16;
-  const int row0 = s.first + place + s0 - s.pos0;
+  const int live = s1 - s0;
+  const int row0 = s.first + place - s.pos0;                 // row of the page's slot 0
+  const size_t head0 = (size_t)pid * C.heads + h0;
+  float* const scales = (value ? C.v_scale : C.k_scale) + head0;
+  uint8_t* const codes = (value ? C.v_codes : C.k_codes) + (head0 << C.page_log2) * C.d;
+  const int head_bytes = C.d << C.page_log2;
+  if (tid < kSlots) s_most[tid] = 0;
+  __syncthreads();
 
-  // the new elements, and their largest magnitude
-  float x[kItems][16];
-  int c0[kItems], c1[kItems];
-  float most = 0.f;
+  // Scale of a head: every thread forms it from s_most; the old codes are brought to it before anybody writes new ones.
+  auto grown = [&](int i, float old) {
+    const float now = scale_for(__builtin_bit_cast(float, s_most[i]));
+    return s0 > 0 && old >= now ? old : now;
+  };
+  auto settle = [&]() {
+    if (s0 > 0) {
+      for (int i = 0; i < heads; ++i) {
+        const float old = scales[i], now = grown(i, old);
+        if (old >= now) continue;
+        const float ratio = old / now;
+        v4u* const held = reinterpret_cast<v4u*>(codes + (size_t)i * head_bytes);
+        for (int j = tid; j < head_bytes / 16; j += threads) {
+          v4u w = held[j];
 #pragma unroll
-  for (int i = 0; i < kItems; ++i) {
-    const int item = tid + i * threads;
-    if (item < live * units) {
-      const int row = row0 + item / units, u = item % units;
-      if (value) {
-        c0[i] = 16 * u;
-        c1[i] = 16 * u + 8;
-        load_unit<BF16>(a.v, row, h, c0[i], c1[i], x[i]);
-      } else {
-        unit_channels(a.rope, u, &c0[i], &c1[i]);
-        load_unit<BF16>(a.k, row, h, c0[i], c1[i], x[i]);
+          for (int e = 0; e < 4; ++e) {
+            const v2f lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[e], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[e], true);
+            w[e] = code4(lo[0] * ratio, lo[1] * ratio, hi[0] * ratio, hi[1] * ratio);
+          }
+          held[j] = w;
+        }
+      }
+    }
+  };
+
+  if (!value) {
+    const int units = C.d / 16, items = live * units;
+    const int rounds = kSlots / a.heads_per_block;           // (token, unit) items of a thread
+    float x[kSlots][16];
+    v4u raw[kSlots][2];
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) {
+      const int round = i % rounds, hh = i / rounds, item = tid + round * threads;
+      if (hh < heads && item < items) {
+        int c0, c1;
+        unit_channels(a.rope, item % units, &c0, &c1);
+        const uint16_t* p = row_of(a.k, row0 + s0 + item / units, h0 + hh);
+        raw[i][0] = load8(p + c0);
+        raw[i][1] = load8(p + c1);
+      }
+    }
+    CosSin cs;
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) {
+      // (slots of a round follow each other in the order of the heads: rounds are 1, 2 or 4 and so are the heads)
+      const int round = i % rounds, hh = i / rounds, item = tid + round * threads;
+      float most = 0.f;
+      if (hh < heads && item < items) {
+        const int u = item % units;
+        widen8<BF16>(raw[i][0], x[i]);
+        widen8<BF16>(raw[i][1], x[i] + 8);
         if (unit_turns(a.rope, u)) {
-          CosSin cs;
-          unit_angles(a.rope, a.batch.n_tokens, row, u, &cs);
+          if (rounds > 1 || i == 0) unit_angles(a.rope, a.batch.n_tokens, row0 + s0 + item / units, u, &cs);
           turn_unit(a.rope, cs, x[i]);
         }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) most = fmaxf(most, magnitude(x[i][j]));
       }
-#pragma unroll
-      for (int j = 0; j < 16; ++j) most = fmaxf(most, __builtin_isfinite(x[i][j]) ? fabsf(x[i][j]) : 0.f);
+      if (hh < heads) fold_most(&s_most[hh], most, false);
     }
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
-  if ((tid & 63) == 0) s_most[tid >> 6] = most;
-  __syncthreads();
-  most = s_most[0];
-  for (int w = 1; w < (threads >> 6); ++w) most = fmaxf(most, s_most[w]);
-
-  const size_t head = (size_t)pid * C.heads + h;
-  float* scale_at = (value ? C.v_scale : C.k_scale) + head;
-  uint8_t* codes = (value ? C.v_codes : C.k_codes) + (head << C.page_log2) * C.d;
-  float scale = scale_for(most);
-  if (s0 > 0) {
-    const float old = *scale_at;
-    if (old >= scale) {
-      scale = old;
-    } else {
-      const float ratio = old / scale;
-      for (int i = tid; i < C.page * C.d / 16; i += threads) {
-        v4u w = reinterpret_cast<v4u*>(codes)[i];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const v2f lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], true);
-          w[j] = code4(lo[0] * ratio, lo[1] * ratio, hi[0] * ratio, hi[1] * ratio);
-        }
-        reinterpret_cast<v4u*>(codes)[i] = w;
-      }
-    }
-    __syncthreads();       // everybody has read the scale; the old codes are in place before the new ones
-  }
-  if (tid == 0) *scale_at = scale;
-
-  const float inv = 1.0f / scale;       // exact: a power of two
-#pragma unroll
-  for (int i = 0; i < kItems; ++i) {
-    const int item = tid + i * threads;
-    if (item >= live * units) continue;
-    const int slot = s0 + item / units;
-    unsigned w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      w[j] = code4(coded(x[i][4 * j], inv), coded(x[i][4 * j + 1], inv), coded(x[i][4 * j + 2], inv),
-                   coded(x[i][4 * j + 3], inv));
-    if (!value) {
-      uint8_t* p = codes + (size_t)slot * C.d;
-      *reinterpret_cast<v2u*>(p + c0[i]) = (v2u){w[0], w[1]};
-      *reinterpret_cast<v2u*>(p + c1[i]) = (v2u){w[2], w[3]};
-    } else if (live < 4) {
-#pragma unroll
-      for (int j = 0; j < 16; ++j) codes[((size_t)(c0[i] + j) << C.page_log2) + slot] = (uint8_t)(w[j / 4] >> (8 * (j % 4)));
-    } else {
-#pragma unroll
-      for (int j = 0; j < 16; ++j) s_turn[(c0[i] + j) * (C.page + 4) + slot] = (uint8_t)(w[j / 4] >> (8 * (j % 4)));
-    }
-  }
-  if (value && live >= 4) {
     __syncthreads();
-    const int quads = C.page / 4;
-    for (int i = tid; i < C.d * quads; i += threads) {
-      const int c = i / quads, t = 4 * (i % quads);
-      const uint8_t* from_lds = s_turn + c * (C.page + 4) + t;
-      uint8_t* p = codes + ((size_t)c << C.page_log2) + t;
-      if (t >= s0 && t + 4 <= s1) {
-        *reinterpret_cast<unsigned*>(p) = *reinterpret_cast<const unsigned*>(from_lds);
-      } else {
-        for (int j = 0; j < 4; ++j)
-          if (t + j >= s0 && t + j < s1) p[j] = from_lds[j];
+    float scale[kSlots];
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) scale[i] = i / rounds < heads ? grown(i / rounds, s0 > 0 ? scales[i / rounds] : 0.f) : 1.f;
+    settle();
+    __syncthreads();                                         // everybody has read the scales, and the old codes are in place
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) {
+      const int round = i % rounds, hh = i / rounds, item = tid + round * threads;
+      if (hh >= heads) continue;
+      if (tid == 0 && round == 0) scales[hh] = scale[i];
+      if (item >= items) continue;
+      const float inv = inverse_of_power(scale[i]);
+      int c0, c1;
+      unit_channels(a.rope, item % units, &c0, &c1);
+      uint8_t* p = codes + (size_t)hh * head_bytes + (size_t)(s0 + item / units) * C.d;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float* y = x[i] + 8 * j;
+        *reinterpret_cast<v2u*>(p + (j ? c1 : c0)) =
+            (v2u){code4(coded(y[0], inv), coded(y[1], inv), coded(y[2], inv), coded(y[3], inv)),
+                  code4(coded(y[4], inv), coded(y[5], inv), coded(y[6], inv), coded(y[7], inv))};
       }
+    }
+    return;
+  }
+
+  const int octets = C.d / 8, quad0 = s0 >> 2, quads = ((s1 + 3) >> 2) - quad0, per_head = quads * octets, items = heads * per_head;
+  const bool spread = (per_head & 63) != 0;
+  float x[kSlots / 2][4][8];
+#pragma unroll
+  for (int i = 0; i < kSlots / 2; ++i) {
+    const int item = tid + i * threads, hh = item / per_head, rest = item - hh * per_head;
+    if (item < items) {
+      const int slot = 4 * (quad0 + rest / octets), c = 8 * (rest % octets);
+      float most = 0.f;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const bool there = slot + t >= s0 && slot + t < s1;
+        const v4u w = there ? load8(row_of(a.v, row0 + slot + t, h0 + hh) + c) : (v4u){0, 0, 0, 0};
+        widen8<BF16>(w, x[i][t]);
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) most = fmaxf(most, magnitude(x[i][t][j]));
+      fold_most(&s_most[hh], most, spread);
+    }
+  }
+  __syncthreads();
+  float scale[kSlots / 2];
+#pragma unroll
+  for (int i = 0; i < kSlots / 2; ++i) {
+    const int item = tid + i * threads, hh = item < items ? item / per_head : 0;
+    scale[i] = grown(hh, s0 > 0 ? scales[hh] : 0.f);
+  }
+  const float first_scale = tid < heads ? grown(tid, s0 > 0 ? scales[tid] : 0.f) : 0.f;
+  settle();
+  __syncthreads();
+  if (tid < heads) scales[tid] = first_scale;
+  const int stride = C.page + 4;
+#pragma unroll
+  for (int i = 0; i < kSlots / 2; ++i) {
+    const int item = tid + i * threads, hh = item / per_head, rest = item - hh * per_head;
+    if (item >= items) continue;
+    const int slot = 4 * (quad0 + rest / octets), c = 8 * (rest % octets);
+    const float inv = inverse_of_power(scale[i]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const unsigned w = code4(coded(x[i][0][j], inv), coded(x[i][1][j], inv), coded(x[i][2][j], inv), coded(x[i][3][j], inv));
+      if (live < 4) {
+        uint8_t* p = codes + (size_t)hh * head_bytes + ((size_t)(c + j) << C.page_log2) + slot;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          if (slot + t >= s0 && slot + t < s1) p[t] = (uint8_t)(w >> (8 * t));
+      } else {
+        *reinterpret_cast<unsigned*>(s_turn + (size_t)(hh * C.d + c + j) * stride + slot) = w;
+      }
+    }
+  }
+  if (live < 4) return;
+  __syncthreads();
+  if (live == C.page) {
+    const int words = C.page / 16;
+    for (int i = tid; i < heads * C.d * words; i += threads) {
+      const int c = i / words, t = 16 * (i % words);         // channel of the heads one after the other
+      const unsigned* from_lds = reinterpret_cast<const unsigned*>(s_turn + (size_t)c * stride + t);
+      *reinterpret_cast<v4u*>(codes + ((size_t)c << C.page_log2) + t) = (v4u){from_lds[0], from_lds[1], from_lds[2], from_lds[3]};
+    }
+    return;
+  }
+  for (int i = tid; i < heads * C.d * quads; i += threads) {
+    const int c = i / quads, t = 4 * (quad0 + i % quads);
+    const uint8_t* from_lds = s_turn + (size_t)c * stride + t;
+    uint8_t* p = codes + ((size_t)c << C.page_log2) + t;
+    if (t >= s0 && t + 4 <= s1) {
+      *reinterpret_cast<unsigned*>(p) = *reinterpret_cast<const unsigned*>(from_lds);
+    } else {
+      for (int j = 0; j < 4; ++j)
+        if (t + j >= s0 && t + j < s1) p[j] = from_lds[j];
     }
   }
 }
@@ -330,23 +431,41 @@ hipError_t launch_append(const PagedCacheArgs& cache, const PagedBatch& batch, b
   a.rope = rope;
   const int bound = batch.max_new < batch.len_bound ? batch.max_new : batch.len_bound;
   a.tasks = (bound + cache.page - 2) / cache.page + 1;       // the new tokens can begin in a page's last slot
-  const int threads = cache.page * cache.d / 16 / kItems < 64 ? 64 : cache.page * cache.d / 16 / kItems;
-  const long long pages = 2ll * batch.batch * cache.heads * a.tasks;
+  const int tokens = bound < cache.page ? bound : cache.page, units = tokens * (cache.d / 16);
+  // Heads to a block: their keys share the angles, but blocks are fewer.  As many as kSlots pieces to a thread allow, while four
+  // blocks are left to a CU.
+  const long long pages = 2ll * batch.batch * a.tasks;
+  int heads = units <= kMostThreads ? kSlots : units <= 2 * kMostThreads ? kSlots / 2 : 1;
+  while (heads > 1 && (heads > cache.heads || pages * ceil_div(cache.heads, heads) < 4 * device_cu_count())) heads /= 2;
+  a.heads_per_block = heads;
+  a.groups = ceil_div(cache.heads, heads);
+  const int rounds = kSlots / heads;                         // a thread's (token, unit) items of the keys
+  int threads = ceil_div(units, rounds);
+  // the values' (head, 4 tokens, 8 channels): a quad more than the tokens fill can be touched
+  const int quads = (tokens + 3) / 4 + (tokens < cache.page ? 1 : 0);
+  const int value_threads = ceil_div(heads * (quads < cache.page / 4 ? quads : cache.page / 4) * (cache.d / 8), kSlots / 2);
+  if (threads < value_threads) threads = value_threads;
+  threads = ceil_div(threads, 64) * 64;
+  const long long page_blocks = pages * a.groups;
   long long q_blocks = 0;
-  if (q_in.heads > 0) {
+  // Queries in the same launch while they are few: of many a kernel of fewer registers turns more (268 MB 46 us, here 59).
+  const bool apart = q_in.heads > 0 && (long long)batch.n_tokens * q_in.heads * cache.d > kQueriesApart;
+  if (q_in.heads > 0 && !apart) {
     a.q = plan_rotate(batch.n_tokens, cache.d, &q_in, &q_out, 1);
     q_blocks = (rotate_threads(a.q) + threads - 1) / threads;
   }
-  if ((pages + q_blocks) * threads >= 1ll << 32) return hipErrorInvalidValue;
-  a.page_blocks = (unsigned)pages;
-  const dim3 grid((unsigned)(pages + q_blocks)), block((unsigned)threads);
-  const size_t lds = (size_t)cache.d * (cache.page + 4);
+  if ((page_blocks + q_blocks) * threads >= 1ll << 32) return hipErrorInvalidValue;
+  a.page_blocks = (unsigned)page_blocks;
+  const dim3 grid((unsigned)(page_blocks + q_blocks)), block((unsigned)threads);
+  const size_t lds = bound < 4 ? 0 : (size_t)heads * cache.d * (cache.page + 4);
   const auto kernel = bf16 ? append_kernel<true> : append_kernel<false>;
   static std::atomic<size_t> raised[2][kPagedDevices];
   const hipError_t e = raise_lds(reinterpret_cast<const void*>(kernel), lds, raised[bf16]);
   if (e != hipSuccess) return e;
   kernel<<<grid, block, lds, stream>>>(a);
-  return hipGetLastError();
+  const hipError_t launched = hipGetLastError();
+  if (launched != hipSuccess || !apart) return launched;
+  return launch_rotate(rope, batch.n_tokens, cache.d, bf16, &q_in, &q_out, 1, stream);
 }
 
 }  // namespace cq

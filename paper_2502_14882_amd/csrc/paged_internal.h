@@ -32,12 +32,13 @@ struct HeadRows {
 };
 
 struct RopeArgs {
+  uint8_t axis_of[128];  // read eight at a time
   const float* inv_freq;
   const int32_t* positions;
   int half;              // pairs; 0: nothing is turned
+  int n_axes;
   int adjacent;          // how they lie
   float sign;            // of the angles
-  uint8_t axis_of[128];
 };
 
 // Raises a kernel's limit of dynamic LDS once per device; `raised` holds what it is on each, and only grows.

@@ -167,9 +167,7 @@ RotateWork plan_rotate(int n_tokens, int d, const HeadRows* in, const HeadRows* 
 long long rotate_threads(const RotateWork& w) { return (long long)w.n_tokens * w.units * w.groups; }
 
 // ---- append
-constexpr int kSlots = 4;          // pieces of 16 elements of the keys that a thread holds, half as many of 32 of the values
 constexpr int kMostThreads = 1024;
-constexpr long long kQueriesApart = 1 << 23;   // elements
 constexpr float kMinScale = 0x1p-100f;
 
 // The smallest power of two s >= 2^-100 with m <= 448 s: 448 = 1.75 * 2^8, so the exponent rises where the
@@ -208,8 +206,11 @@ __device__ inline void fold_most(unsigned* most, float x, bool spread) {
 
 // One page of a sequence, heads_per_block heads of the keys or of the values.
 //   keys:   thread -> (token, 16 channels that hold whole pairs), a slot per head: the angles serve all of them
+// kSlots: pieces of 16 elements of the keys that a thread holds, half as many of 32 of the values.  Two leave six waves to a SIMD, with
+// which queries are turned in the same launch in the time of a kernel of their own; four, for pages of over 32768 elements, four
+// (and took 2 % longer where both can be had).
 //   values: thread -> (head, 4 tokens, 8 channels): a channel's four codes are one word, which turn in LDS
-template <bool BF16>
+template <int kSlots, bool BF16>
 __global__ void __launch_bounds__(kMostThreads) append_kernel(AppendArgs a) {
   extern __shared__ __align__(16) uint8_t s_turn[];          // values: [heads][d][page + 4]
   __shared__ unsigned s_most[kSlots];
@@ -432,25 +433,24 @@ hipError_t launch_append(const PagedCacheArgs& cache, const PagedBatch& batch, b
   const int bound = batch.max_new < batch.len_bound ? batch.max_new : batch.len_bound;
   a.tasks = (bound + cache.page - 2) / cache.page + 1;       // the new tokens can begin in a page's last slot
   const int tokens = bound < cache.page ? bound : cache.page, units = tokens * (cache.d / 16);
-  // Heads to a block: their keys share the angles, but blocks are fewer.  As many as kSlots pieces to a thread allow, while four
-  // blocks are left to a CU.
+  // Heads to a block: their keys share the angles, but blocks are fewer.  As many as the slots allow, while four blocks are
+  // left to a CU.
   const long long pages = 2ll * batch.batch * a.tasks;
-  int heads = units <= kMostThreads ? kSlots : units <= 2 * kMostThreads ? kSlots / 2 : 1;
+  const int slots = units <= 2 * kMostThreads ? 2 : 4;
+  int heads = units <= kMostThreads ? slots : 1;
   while (heads > 1 && (heads > cache.heads || pages * ceil_div(cache.heads, heads) < 4 * device_cu_count())) heads /= 2;
   a.heads_per_block = heads;
   a.groups = ceil_div(cache.heads, heads);
-  const int rounds = kSlots / heads;                         // a thread's (token, unit) items of the keys
+  const int rounds = slots / heads;                          // a thread's (token, unit) items of the keys
   int threads = ceil_div(units, rounds);
   // the values' (head, 4 tokens, 8 channels): a quad more than the tokens fill can be touched
   const int quads = (tokens + 3) / 4 + (tokens < cache.page ? 1 : 0);
-  const int value_threads = ceil_div(heads * (quads < cache.page / 4 ? quads : cache.page / 4) * (cache.d / 8), kSlots / 2);
+  const int value_threads = ceil_div(heads * (quads < cache.page / 4 ? quads : cache.page / 4) * (cache.d / 8), slots / 2);
   if (threads < value_threads) threads = value_threads;
   threads = ceil_div(threads, 64) * 64;
   const long long page_blocks = pages * a.groups;
   long long q_blocks = 0;
-  // Queries in the same launch while they are few: of many a kernel of fewer registers turns more (268 MB 46 us, here 59).
-  const bool apart = q_in.heads > 0 && (long long)batch.n_tokens * q_in.heads * cache.d > kQueriesApart;
-  if (q_in.heads > 0 && !apart) {
+  if (q_in.heads > 0) {
     a.q = plan_rotate(batch.n_tokens, cache.d, &q_in, &q_out, 1);
     q_blocks = (rotate_threads(a.q) + threads - 1) / threads;
   }
@@ -458,14 +458,13 @@ hipError_t launch_append(const PagedCacheArgs& cache, const PagedBatch& batch, b
   a.page_blocks = (unsigned)page_blocks;
   const dim3 grid((unsigned)(page_blocks + q_blocks)), block((unsigned)threads);
   const size_t lds = bound < 4 ? 0 : (size_t)heads * cache.d * (cache.page + 4);
-  const auto kernel = bf16 ? append_kernel<true> : append_kernel<false>;
-  static std::atomic<size_t> raised[2][kPagedDevices];
-  const hipError_t e = raise_lds(reinterpret_cast<const void*>(kernel), lds, raised[bf16]);
+  const auto kernel = slots == 2 ? (bf16 ? append_kernel<2, true> : append_kernel<2, false>)
+                                 : (bf16 ? append_kernel<4, true> : append_kernel<4, false>);
+  static std::atomic<size_t> raised[4][kPagedDevices];
+  const hipError_t e = raise_lds(reinterpret_cast<const void*>(kernel), lds, raised[(slots == 2 ? 2 : 0) + bf16]);
   if (e != hipSuccess) return e;
   kernel<<<grid, block, lds, stream>>>(a);
-  const hipError_t launched = hipGetLastError();
-  if (launched != hipSuccess || !apart) return launched;
-  return launch_rotate(rope, batch.n_tokens, cache.d, bf16, &q_in, &q_out, 1, stream);
+  return hipGetLastError();
 }
 
 }  // namespace cq

@@ -1,25 +1,40 @@
 // Attention over the paged e4m3 cache for many query rows per KV head: prompts, and pieces of them.
 //
-// Rows: the (new token, query head) pairs of one KV head, 32 to a tile of the matrix cores, kRowTiles tiles to a wave, four waves
-// to a workgroup.  For 64 tokens at a time:
+// Rows: the (new token, query head) pairs of one KV head, 32 to a wave as columns of its products.  For 64 tokens at a time:
 //     S^T = K Q^T      A = keys (token rows), B = queries                    v_mfma_f32_32x32x16_f16
 //     p = exp2(s - m)  with the row's running reference m and sum l
 //     O^T += V^T P^T   A = values (channel rows), B = weights
-// Bound: the matrix cores, 4 d flops for each pair of a row and a token.  What keeps them fed:
+// Bound: the matrix cores, 4 d flops for each pair of a row and a token - or rather the chip's power: with zeros for inputs the
+// same instructions take a fifth less time (a plain matrix product of 8192 x 8192 x 8192 a quarter less).  What keeps the cores fed:
 //   - the codes are turned into fp16 once per workgroup, on their way into LDS (exactly: a code has four significant bits), and
-//     lie there operand by operand (1 KB, lane by lane), so that an operand is one linear 16-byte read per lane; each is used for two
-//     products (two row tiles) - with one the LDS would bound;
+//     lie there operand by operand (1 KB, lane by lane), so that an operand is one linear 16-byte read per lane;
 //   - which token is which row of S^T is chosen such that the weights a lane has computed are its operand of the second product:
 //     token 16 u + 8 f + 4 j + b of 32 is row 16 u + 8 j + 4 f + b, f being the half of the wave;
-//   - two tiles of keys, two of values and the next codes in registers are under way at once: while a wave turns the
-//     logits of one step into weights, its products with the next step's keys are in the matrix cores; one barrier a step;
+//   - products, softmax and the codes' way into LDS are interleaved within a wave (half_step): a wave whose next product waits
+//     for the cores also keeps the other wave's vector instructions waiting (one wave with 16 products and one with 64 adds
+//     take the sum of their times), while vector instructions between two products of a wave cost next to nothing - except
+//     v_dot2, which runs on the cores, so the weights are summed by additions;
 //   - m follows a row's largest logit only when that is more than 2^8 above it (weights up to 256 fit fp16 as well as those
 //     up to 1), so that O is rescaled a few times per row and not at every step.
-// The sum l is taken of the rounded weights, which takes their common error out of the result.
+// Two row tiles per wave and one wave to a SIMD read half as much from LDS, but took 850 us where this takes 589 (8192 rows of 32 heads
+// over 8192 tokens, 128 channels): the accumulators then travel between the two register files.
+#include <type_traits>
+#include <utility>
+
 #include "paged_device.h"
 
 namespace cq {
 namespace {
+
+// f(std::integral_constant<int, 0>{}) .. of N: loops whose index the body needs at compile time
+template <class F, int... I>
+__device__ inline void static_for_each(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ inline void static_for(F&& f) {
+  static_for_each(f, std::make_integer_sequence<int, N>{});
+}
 
 template <int D>
 struct Prompt {
@@ -211,23 +226,31 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads) prompt_kernel(PagedAttent
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[c][e] = 0.f;
 
-  // Half h of the sequence of halves of steps (32 tokens each).  Three things that do not depend on each other, dealt out in
-  // kOps groups such that the matrix cores work under the softmax: the logits of half h + 1 (`next`), the weights of half h (from `now`, to
-  // `p`), and the products of half h - 1's weights (`before`) with its values.
-  auto half_step = [&](const uint8_t* keys, const uint8_t* values, int step, int t, const Groups& w, v16f& now, v16f& next, v8h (&p)[2],
-                       v8h (&before)[2]) {
-    auto key_op = [&](int j) { return *reinterpret_cast<const v8h*>(keys + j * T::kKeyStride); };
-    // in the order [16 tokens][32 channels]; in LDS the four operands of 32 channels lie together
-    auto value_op = [&](int j) {
-      return *reinterpret_cast<const v8h*>(values + (j % T::kValueTiles * 4 + j / T::kValueTiles) * T::kValueStride);
-    };
-    constexpr int kAhead = 2;
-    v8h k[kAhead + 1], v[kAhead + 1];
+  // The largest of each group's eight logits (raw) of a lane.
+  auto largest = [&](const v16f& sc, float (&best)[2]) {
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      k[j] = key_op(j);
-      v[j] = value_op(j);
+    for (int i = 0; i < 2; ++i) {
+      best[i] = fmaxf(sc[8 * i], sc[8 * i + 1]);
+#pragma unroll
+      for (int e = 2; e < 8; e += 2) best[i] = fmaxf(fmaxf(best[i], sc[8 * i + e]), sc[8 * i + e + 1]);
     }
+  };
+  // Half h of the sequence of halves of steps (32 tokens each).  Things that do not depend on each other are dealt out in groups of
+  // two products each, so that the vector unit works under the matrix cores: a wave whose next product waits for the cores keeps the
+  // other wave's vector instructions waiting too, so the overlap has to be within a wave.
+  //   logits of half h + 1 (`next`) | most of the weights of half h (from `now`, to `p`), and what `beside` does
+  //   products of half h - 1's weights (`before`) with its values | the other weights, the largest of `next`
+  auto half_step = [&](const uint8_t* keys, const uint8_t* values, int step, int t, const Groups& w, v16f& now, float (&best)[2], v16f& next,
+                       v8h (&p)[2], v8h (&before)[2], auto&& beside) {
+    // operands in the order [keys: 16 channels] [values: 16 tokens][32 channels]; in LDS the four value operands of 32 channels lie together
+    auto op = [&](auto J) {
+      constexpr int j = decltype(J)::value, v = j - T::kOps;
+      if constexpr (v < 0) return *reinterpret_cast<const v8h*>(keys + j * T::kKeyStride);
+      else return *reinterpret_cast<const v8h*>(values + (v % T::kValueTiles * 4 + v / T::kValueTiles) * T::kValueStride);
+    };
+    constexpr int kAhead = 4;                                         // operands on their way from LDS
+    v8h ring[kAhead];
+    static_for<kAhead>([&](auto J) { ring[decltype(J)::value] = op(J); });
     __builtin_amdgcn_sched_barrier(0);
     if (step * kStep + kStep > block_lo || __any(w.pid < 0)) {        // where store_values looks for NaN codes
       const unsigned long long there = __ballot(w.pid >= 0) >> (2 * t);      // bit i: group i
@@ -244,23 +267,22 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads) prompt_kernel(PagedAttent
         }
         __builtin_amdgcn_sched_barrier(0);                            // (all comparisons at once would not fit the scalar registers)
       }
+      largest(now, best);
     }
     float f[2], top = kNoMax;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       f[i] = row_scale * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w.ks), 2 * t + i));
-      float best = now[8 * i];
-#pragma unroll
-      for (int e = 1; e < 8; ++e) best = fmaxf(best, now[8 * i + e]);
-      top = fmaxf(top, best * f[i]);
+      top = fmaxf(top, best[i] * f[i]);
     }
     if (__any(top > m + 8.f)) {
       // the weights before are relative to the old reference: their products are added first
-#pragma unroll
-      for (int j = 0; j < T::kOps; ++j) {
-        acc[j % T::kValueTiles] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value_op(j), before[j / T::kValueTiles], acc[j % T::kValueTiles], 0, 0, 0);
+      static_for<T::kOps>([&](auto J) {
+        constexpr int j = decltype(J)::value, c = j % T::kValueTiles;
+        const v8h o = op(std::integral_constant<int, T::kOps + j>{});
+        acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o, before[j / T::kValueTiles], acc[c], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
-      }
+      });
 #pragma unroll
       for (int i = 0; i < 2; ++i) before[i] = (v8h){0, 0, 0, 0, 0, 0, 0, 0};
       top = fmaxf(top, __shfl_xor(top, 32));
@@ -272,28 +294,39 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads) prompt_kernel(PagedAttent
     }
 #pragma unroll
     for (int e = 0; e < 16; ++e) next[e] = 0.f;
-#pragma unroll
-    for (int j = 0; j < T::kOps; ++j) {
-      if (j + kAhead < T::kOps) {
-        k[(j + kAhead) % (kAhead + 1)] = key_op(j + kAhead);
-        v[(j + kAhead) % (kAhead + 1)] = value_op(j + kAhead);
+    __builtin_amdgcn_s_setprio(1);
+    constexpr int kUnder = T::kOps > 2 ? 6 : 8;                       // pairs of weights under the logits, of 8
+    static_for<2 * T::kOps>([&](auto J) {
+      constexpr int j = decltype(J)::value;
+      const v8h o = ring[j % kAhead];
+      if constexpr (j + kAhead < 2 * T::kOps) ring[j % kAhead] = op(std::integral_constant<int, j + kAhead>{});
+      if constexpr (j < T::kOps) {
+        next = __builtin_amdgcn_mfma_f32_32x32x16_f16(o, q[j], next, 0, 0, 0);
+      } else {
+        constexpr int v = j - T::kOps, c = v % T::kValueTiles;
+        acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o, before[v / T::kValueTiles], acc[c], 0, 0, 0);
       }
-      if (j == 0) __builtin_amdgcn_s_setprio(1);
-      next = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[j % (kAhead + 1)], q[j], next, 0, 0, 0);
-      acc[j % T::kValueTiles] =
-          __builtin_amdgcn_mfma_f32_32x32x16_f16(v[j % (kAhead + 1)], before[j / T::kValueTiles], acc[j % T::kValueTiles], 0, 0, 0);
-#pragma unroll
-      for (int pair = 8 * j / T::kOps; pair < 8 * (j + 1) / T::kOps; ++pair) {
-        const int i = pair >> 2, e = 2 * pair;
-        const float x = exp2_fast(__builtin_fmaf(now[e], f[i], -m)), y = exp2_fast(__builtin_fmaf(now[e + 1], f[i], -m));
-        v2h two = {(_Float16)x, (_Float16)y};
-        asm volatile("" : "+v"(two));        // here, and not where the next half uses it
-        l = __builtin_amdgcn_fdot2(two, (v2h){(_Float16)1.f, (_Float16)1.f}, l, false);
-        p[i][e & 7] = two[0];
-        p[i][(e & 7) + 1] = two[1];
+      if constexpr (j % 2 == 1) {                                     // behind every second product
+        constexpr int groups = T::kOps / 2, group = j / 2;
+        constexpr int at = group % groups, base = group < groups ? 0 : kUnder, many = group < groups ? kUnder : 8 - kUnder;
+        constexpr int first = base + many * at / groups, last = base + many * (at + 1) / groups;
+        static_for<last - first>([&](auto P) {
+          constexpr int pair = first + decltype(P)::value, i = pair / 4, e = 2 * pair;
+          const float x = exp2_fast(__builtin_fmaf(now[e], f[i], -m)), y = exp2_fast(__builtin_fmaf(now[e + 1], f[i], -m));
+          v2h two = {(_Float16)x, (_Float16)y};
+          asm volatile("" : "+v"(two));      // here, and not where the next half uses it
+          l += x + y;
+          p[i][e & 7] = two[0];
+          p[i][(e & 7) + 1] = two[1];
+        });
+        beside(group);
+        if constexpr (j == 2 * T::kOps - 1) {
+          largest(next, best);
+          asm volatile("" : "+v"(best[0]), "+v"(best[1]));
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    });
     __builtin_amdgcn_s_setprio(0);
   };
 
@@ -327,18 +360,20 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads) prompt_kernel(PagedAttent
     int pid = page_of(at(3));
     __syncthreads();
     v16f sc0, sc1;
+    float best[2];
     v8h p0[2], p1[2];
 #pragma unroll
     for (int e = 0; e < 16; ++e) sc0[e] = 0.f;
 #pragma unroll
     for (int j = 0; j < T::kOps; ++j)
       sc0 = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const v8h*>(keys_of(0, 0) + j * T::kKeyStride), q[j], sc0, 0, 0, 0);
+    largest(sc0, best);
 #pragma unroll
     for (int i = 0; i < 2; ++i) p1[i] = (v8h){0, 0, 0, 0, 0, 0, 0, 0};
     acc_unit = unit;
     for (int i = 0; i < steps; ++i) {
       if (at(i) * kStep + kStep > block_lo || __any(g0.pid < 0)) __syncthreads();        // s_nan of this step
-      half_step(keys_of(i, 1), values_of(i + 1, 1), at(i), 0, g0, sc0, sc1, p0, p1);     // values_of(i - 1, 1): the same buffer
+      half_step(keys_of(i, 1), values_of(i + 1, 1), at(i), 0, g0, sc0, best, sc1, p0, p1, [](int) {});   // values_of(i - 1, 1): the same buffer
       __syncthreads();
       if (tid < 2) s_nan[(step0 + i + 2) % 3][tid] = 0;               // last read a step ago
       if (unit != acc_unit) {
@@ -347,15 +382,19 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads) prompt_kernel(PagedAttent
         for (int c = 0; c < T::kValueTiles; ++c) acc[c] *= f;
         acc_unit = unit;
       }
-      if (i + 1 < steps) {
-        unit = unit_of(unit, g1);
-        store_values((i + 1) & 1, at(i + 1), g1, unit);
-        if (i + 2 < steps) store_keys(i & 1);
-      }
-      load_scales(&g2);
-      load_values(at(i + 2), g2.pid);
-      load_keys(at(i + 3), pid);
-      half_step(keys_of(i + 1, 0), values_of(i, 0), at(i), 1, g0, sc1, sc0, p1, p0);
+      if (i + 1 < steps) unit = unit_of(unit, g1);
+      half_step(keys_of(i + 1, 0), values_of(i, 0), at(i), 1, g0, sc1, best, sc0, p1, p0, [&](int group) {
+        // (beyond the last step the last one's codes again, which nobody reads)
+        if (group == 0) {
+          store_values((i + 1) & 1, at(i + 1), g1, unit);
+          load_values(at(i + 2), g2.pid);
+        }
+        if (group == (T::kOps > 2 ? 1 : 0)) {
+          store_keys(i & 1);
+          load_keys(at(i + 3), pid);
+          load_scales(&g2);
+        }
+      });
       g0 = g1;
       g1 = g2;
       g2.pid = pid;

@@ -149,6 +149,7 @@ int cqp_rotate(const cqp_rope_t* rope, const int32_t* positions, int32_t n_token
   if (backward) r.sign = -1.0f;
   const hipError_t e = cq::launch_rotate(r, n_tokens, head_dim, dtype == CQP_BF16, from, to, n_tensors,
                                          static_cast<hipStream_t>(stream));
+  if (e == hipErrorInvalidConfiguration) return fail(CQ_ERR_SHAPE, "%d tokens are too many for a launch", n_tokens);
   return e == hipSuccess ? CQ_OK : hip_fail(e, "rotate");
 }
 
@@ -178,6 +179,7 @@ int cqp_append_kv(const cqp_cache_t* cache, const cqp_batch_t* batch, int32_t n_
   if (n_tokens == 0) return CQ_OK;
   const hipError_t e = cq::launch_append(c, s, dtype == CQP_BF16, rows_of(*k), rows_of(*v), r, from, to,
                                          static_cast<hipStream_t>(stream));
+  if (e == hipErrorInvalidConfiguration) return fail(CQ_ERR_SHAPE, "%d tokens in %d sequences are too many for a launch", n_tokens, s.batch);
   return e == hipSuccess ? CQ_OK : hip_fail(e, "append");
 }
 
@@ -187,7 +189,8 @@ size_t cqp_attn_workspace_bytes(const cqp_cache_t* cache, const cqp_batch_t* bat
   if (check_cache(cache, false, &c) != CQ_OK || n_tokens < 0 || check_batch(batch, c, n_tokens, false, &s) != CQ_OK ||
       n_q_heads < 1 || n_q_heads % c.heads != 0)
     return 0;
-  return cq::make_paged_plan(c, s, n_q_heads).ws_bytes;
+  const cq::PagedPlan plan = cq::make_paged_plan(c, s, n_q_heads);
+  return plan.fits ? plan.ws_bytes : 0;
 }
 
 int cqp_attn(const cqp_cache_t* cache, const cqp_batch_t* batch, int32_t n_tokens, int32_t dtype, const cqp_heads_t* q,
@@ -208,6 +211,7 @@ int cqp_attn(const cqp_cache_t* cache, const cqp_batch_t* batch, int32_t n_token
     return fail(CQ_ERR_SHAPE, "softmax_scale must be finite and >= 0");
   if (softmax_scale == 0.f) softmax_scale = 1.0f / std::sqrt((float)a.cache.d);
   a.plan = cq::make_paged_plan(a.cache, a.batch, q->n_heads);
+  if (!a.plan.fits) return fail(CQ_ERR_SHAPE, "%d tokens of %d heads in %d sequences are too many for a launch", n_tokens, q->n_heads, batch->batch);
   if (!workspace) return fail(CQ_ERR_WORKSPACE, "workspace is NULL");
   if (!aligned(workspace, 256)) return fail(CQ_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   if (workspace_bytes < a.plan.ws_bytes)

@@ -109,6 +109,7 @@ __device__ inline v4u load8(const uint16_t* p) { return *reinterpret_cast<const 
 // Thread -> (token, group of heads, unit), units fastest.  The heads of two tensors are counted through.
 struct RotateWork {
   HeadRows in[2], out[2];
+  const int32_t *from, *to;     // NULL, or where the device keeps the first token and the end of those that are turned
   int n_tokens, units, heads_per_thread, groups;
 };
 
@@ -118,7 +119,7 @@ __device__ inline void rotate_thread(const RopeArgs& rope, const RotateWork& w, 
   const long long rest = i / w.units;
   const int group = (int)(rest % w.groups);
   const long long token = rest / w.groups;
-  if (token >= w.n_tokens) return;
+  if (token >= w.n_tokens || (w.from && (token < *w.from || token >= *w.to))) return;
   const int heads = w.in[0].heads + w.in[1].heads;
   const int h0 = group * w.heads_per_thread;
   const int h1 = h0 + w.heads_per_thread < heads ? h0 + w.heads_per_thread : heads;
@@ -184,7 +185,7 @@ struct AppendArgs {
   PagedBatch batch;
   HeadRows k, v;
   RotateWork q;
-  int tasks;               // pages that a sequence's new tokens can reach
+  int one_each;            // every sequence's new token lies in one page
   int heads_per_block, groups;
   unsigned page_blocks;    // workgroups for pages; those behind turn queries
 };
@@ -226,13 +227,18 @@ __global__ void __launch_bounds__(kMostThreads) append_kernel(AppendArgs a) {
   const int h0 = (int)(id % (unsigned)a.groups) * a.heads_per_block;
   const int heads = C.heads - h0 < a.heads_per_block ? C.heads - h0 : a.heads_per_block;
   id /= (unsigned)a.groups;
-  const int task = (int)(id % (unsigned)a.tasks), b = (int)(id / (unsigned)a.tasks);
+  // the sequence's places [from, to) that have a new row, and the pages that they lie in
+  auto pages_of = [&](const Sequence& s) {
+    const int from = s.pos0 > 0 ? s.pos0 : 0, to = s.pos0 + s.n;
+    return to <= from ? 0 : ((to - 1) >> C.page_log2) - (from >> C.page_log2) + 1;
+  };
+  const Item item = a.one_each ? Item{(int)id, 0} : a.batch.batch == 1 ? Item{0, (int)id} : locate(a.batch, (int)id, pages_of);
+  if (item.b < 0) return;
+  const int b = item.b;
   const Sequence s = load_sequence(a.batch, b);
-  if (s.n == 0) return;
-  // the sequence's places [from, to) that have a new row
+  if (item.local >= pages_of(s)) return;
   const int from = s.pos0 > 0 ? s.pos0 : 0, to = s.pos0 + s.n;
-  const int index = (from >> C.page_log2) + task, place = index << C.page_log2;
-  if (place >= to || to <= from) return;
+  const int index = (from >> C.page_log2) + item.local, place = index << C.page_log2;
   const int pid = a.batch.page_table[(size_t)b * a.batch.max_pages + index];      // place < to <= len: within the row
   if ((unsigned)pid >= (unsigned)C.n_pages) return;
   const int s0 = from > place ? from - place : 0, s1 = to - place < C.page ? to - place : C.page;
@@ -415,7 +421,7 @@ hipError_t launch_rotate(const RopeArgs& rope, int n_tokens, int d, bool bf16, c
                          int n_tensors, hipStream_t stream) {
   const RotateWork w = plan_rotate(n_tokens, d, in, out, n_tensors);
   const long long blocks = (rotate_threads(w) + 255) / 256;
-  if (blocks >= 1ll << 24) return hipErrorInvalidValue;      // 2^32 threads
+  if (blocks >= 1ll << 24) return hipErrorInvalidConfiguration;      // 2^32 threads
   if (bf16) rotate_kernel<true><<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(rope, w);
   else rotate_kernel<false><<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(rope, w);
   return hipGetLastError();
@@ -431,11 +437,14 @@ hipError_t launch_append(const PagedCacheArgs& cache, const PagedBatch& batch, b
   a.v = v;
   a.rope = rope;
   const int bound = batch.max_new < batch.len_bound ? batch.max_new : batch.len_bound;
-  a.tasks = (bound + cache.page - 2) / cache.page + 1;       // the new tokens can begin in a page's last slot
+  a.one_each = bound == 1;
+  // pages that a sequence's new tokens can reach (they can begin in a page's last slot), and those that all tokens can
+  const long long each = (bound + cache.page - 2) / cache.page + 1, most = each * batch.batch;
+  const long long by_tokens = (long long)batch.n_tokens / cache.page + 2ll * batch.batch;
+  const long long pages = 2 * (by_tokens < most ? by_tokens : most);     // keys and values
   const int tokens = bound < cache.page ? bound : cache.page, units = tokens * (cache.d / 16);
   // Heads to a block: their keys share the angles, but blocks are fewer.  As many as the slots allow, while four blocks are
   // left to a CU.
-  const long long pages = 2ll * batch.batch * a.tasks;
   const int slots = units <= 2 * kMostThreads ? 2 : 4;
   int heads = units <= kMostThreads ? slots : 1;
   while (heads > 1 && (heads > cache.heads || pages * ceil_div(cache.heads, heads) < 4 * device_cu_count())) heads /= 2;
@@ -452,9 +461,11 @@ hipError_t launch_append(const PagedCacheArgs& cache, const PagedBatch& batch, b
   long long q_blocks = 0;
   if (q_in.heads > 0) {
     a.q = plan_rotate(batch.n_tokens, cache.d, &q_in, &q_out, 1);
+    a.q.from = batch.q_start;
+    a.q.to = batch.q_start + batch.batch;
     q_blocks = (rotate_threads(a.q) + threads - 1) / threads;
   }
-  if ((page_blocks + q_blocks) * threads >= 1ll << 32) return hipErrorInvalidValue;
+  if ((page_blocks + q_blocks) * threads >= 1ll << 32) return hipErrorInvalidConfiguration;
   a.page_blocks = (unsigned)page_blocks;
   const dim3 grid((unsigned)(page_blocks + q_blocks)), block((unsigned)threads);
   const size_t lds = bound < 4 ? 0 : (size_t)heads * cache.d * (cache.page + 4);

@@ -21,10 +21,7 @@ struct Sequence {
   int len;     // tokens in the cache
 };
 __device__ inline int clamp_int(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
-__device__ inline Sequence load_sequence(const PagedBatch& s, int b) {
-  // the same for all lanes (b is), and known to be to the compiler: branches on them are scalar
-  const int from = __builtin_amdgcn_readfirstlane(s.q_start[b]), to = __builtin_amdgcn_readfirstlane(s.q_start[b + 1]);
-  const int len = __builtin_amdgcn_readfirstlane(s.seq_lens[b]);
+__device__ inline Sequence sequence_of(const PagedBatch& s, int from, int to, int len) {
   Sequence q;
   q.first = clamp_int(from, 0, s.n_tokens);
   const int rows = clamp_int(to, q.first, s.n_tokens) - q.first;
@@ -32,6 +29,38 @@ __device__ inline Sequence load_sequence(const PagedBatch& s, int b) {
   q.len = clamp_int(len, 0, s.len_bound);
   q.pos0 = q.len - rows;
   return q;
+}
+// b is the same for all lanes, and the result is known to be to the compiler: branches on it are scalar
+__device__ inline Sequence load_sequence(const PagedBatch& s, int b) {
+  return sequence_of(s, __builtin_amdgcn_readfirstlane(s.q_start[b]), __builtin_amdgcn_readfirstlane(s.q_start[b + 1]),
+                     __builtin_amdgcn_readfirstlane(s.seq_lens[b]));
+}
+
+// Work items counted through the sequences, count(sequence) of each: whose the item `index` is, and which of its items; sequence -1: there
+// are not as many.  A launch then needs workgroups for the items that the tokens can make, not for the most of every sequence.
+struct Item {
+  int b, local;
+};
+template <class F>
+__device__ inline Item locate(const PagedBatch& s, int index, F count) {
+  const int lane = threadIdx.x & 63;
+  for (int base = 0; base < s.batch; base += 64) {
+    const int b = base + lane;
+    const int own = b < s.batch ? count(sequence_of(s, s.q_start[b], s.q_start[b + 1], s.seq_lens[b])) : 0;
+    int sum = own;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int x = __shfl_up(sum, o);
+      if (lane >= o) sum += x;
+    }
+    const int all = __builtin_amdgcn_readlane(sum, 63);
+    if (index < all) {
+      const int at = __builtin_ctzll(__ballot(sum > index));
+      return {base + at, index - __builtin_amdgcn_readlane(sum - own, at)};
+    }
+    index -= all;
+  }
+  return {-1, 0};
 }
 
 // ---- 16-bit elements, eight of them as they lie in memory

@@ -410,12 +410,14 @@ template <int D, bool BF16>
 __global__ void __launch_bounds__(256) combine_splits_kernel(PagedAttention a) {
   constexpr int kPer = (D + 63) / 64;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  unsigned long long id = (unsigned long long)blockIdx.x * 4 + wave;
-  const int hq = (int)(id % (unsigned)a.q.heads);
-  id /= (unsigned)a.q.heads;
-  const int i = (int)(id % (unsigned)a.batch.max_new), b = (int)(id / (unsigned)a.batch.max_new);
-  if (b >= a.batch.batch) return;
-  const Sequence s = load_sequence(a.batch, b);
+  const unsigned long long id = (unsigned long long)blockIdx.x * 4 + wave;
+  const int hq = (int)(id % (unsigned)a.q.heads), at = (int)(id / (unsigned)a.q.heads);      // row of the tokens
+  const int first_row = clamp_int(__builtin_amdgcn_readfirstlane(a.batch.q_start[0]), 0, a.batch.n_tokens);
+  if (at < first_row) return;
+  const Item item = locate(a.batch, at - first_row, [&](const Sequence& s) { return s.len - s.pos0; });      // all rows of a sequence
+  if (item.b < 0) return;
+  const int i = item.local;
+  const Sequence s = load_sequence(a.batch, item.b);
   const bool few = a.plan.few && (!a.plan.prompts || s.n * a.g <= kFewRows);
   if (few && a.plan.few_joins) return;
   const int split_steps = few ? a.plan.split_steps : a.plan.prompt_split_steps;
@@ -457,7 +459,6 @@ __global__ void __launch_bounds__(256) combine_splits_kernel(PagedAttention a) {
 template <int D, int NT>
 hipError_t launch_few(const PagedAttention& a, bool bf16, hipStream_t stream) {
   const long long blocks = (long long)a.batch.batch * a.cache.heads * a.plan.row_blocks * a.plan.few_splits;
-  if (blocks >= 1ll << 24) return hipErrorInvalidValue;      // 2^32 threads
   const size_t lds = (size_t)kWaves * 16 * NT * (D + 4) * sizeof(float);
   const auto kernel = bf16 ? few_kernel<D, NT, true> : few_kernel<D, NT, false>;
   static std::atomic<size_t> raised[2][kPagedDevices];
@@ -474,9 +475,7 @@ hipError_t launch_few_d(const PagedAttention& a, bool bf16, hipStream_t stream) 
 
 template <int D>
 hipError_t launch_combine_d(const PagedAttention& a, bool bf16, hipStream_t stream) {
-  const long long rows = (long long)a.batch.batch * a.batch.max_new * a.q.heads;
-  const long long blocks = (rows + 3) / 4;
-  if (blocks >= 1ll << 24) return hipErrorInvalidValue;
+  const long long blocks = ((long long)a.batch.n_tokens * a.q.heads + 3) / 4;
   if (bf16) combine_splits_kernel<D, true><<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(a);
   else combine_splits_kernel<D, false><<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(a);
   return hipGetLastError();
@@ -521,8 +520,10 @@ PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, 
   }
   if (p.prompts) {
     const int block = prompt_rows(cache.d);
-    p.prompt_blocks = (int)((rows + block - 1) / block);
-    const long long beside = (long long)batch.batch * cache.heads * p.prompt_blocks;
+    // all tokens' rows in whole blocks, and one begun for each sequence; of one sequence, or of even ones, what the longest takes
+    const long long most_blocks = (rows + block - 1) / block * batch.batch, token_blocks = (long long)batch.n_tokens * g / block + batch.batch;
+    p.prompt_blocks = (int)(token_blocks < most_blocks ? token_blocks : most_blocks);
+    const long long beside = (long long)cache.heads * p.prompt_blocks;
     const long long most = steps / 8 < 32 ? steps / 8 : 32;
     int best = 1;
     double best_full = 0;
@@ -546,6 +547,10 @@ PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, 
     p.ws_bytes = ((p.ws_acc_floats + parts * cache.d) * sizeof(float) + 255) / 256 * 256;
     if (p.ws_bytes == 0) p.ws_bytes = 256;
   }
+  // what a launch takes: 2^32 threads
+  p.fits = rows < 1ll << 30 && (!p.few || (long long)batch.batch * cache.heads * p.row_blocks * p.few_splits < 1ll << 24) &&
+           (!p.prompts || (long long)cache.heads * p.prompt_blocks * p.prompt_splits < 1ll << 23) &&
+           (long long)batch.n_tokens * n_q_heads < 1ll << 26;
   return p;
 }
 

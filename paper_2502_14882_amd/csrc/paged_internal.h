@@ -78,11 +78,12 @@ struct PagedPlan {
   int split_steps = 1;     // its steps of kStep tokens per split of a sequence
   int few_splits = 1;      // of the longest sequence
   bool few_joins = false;  // it joins them itself
-  int prompt_blocks = 1;   // the same of the second kernel
+  int prompt_blocks = 1;   // blocks of rows of the second kernel, of all sequences
   int prompt_split_steps = 1, prompt_splits = 1;
   int splits = 1;          // the larger number of splits
   size_t ws_ml_floats = 0, ws_acc_floats = 0;   // workspace: [counts | m, l | acc], the latter two [rows][splits]
   size_t ws_bytes = 256;
+  bool fits = true;        // every launch has a size that launches take
 };
 int prompt_rows(int d);    // rows of a workgroup of the second kernel
 PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, int n_q_heads);

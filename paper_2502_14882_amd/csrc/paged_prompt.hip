@@ -38,7 +38,7 @@ __device__ inline void static_for(F&& f) {
 
 template <int D>
 struct Prompt {
-  static constexpr int kWaves = D <= 160 ? 8 : 4;                     // two to a SIMD while 256 registers hold what one needs
+  static constexpr int kWaves = D <= 192 ? 8 : 4;                     // two to a SIMD while 256 registers hold what one needs
   static constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves;
   static constexpr int kOps = D / 16;                                 // operands of 32 keys, and of 32 tokens' values
   static constexpr int kValueTiles = D / 32;
@@ -74,13 +74,18 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads) prompt_kernel(PagedAttent
   unsigned id = blockIdx.x;
   const int h = (int)(id % (unsigned)C.heads);
   id /= (unsigned)C.heads;
-  const int b = (int)(id % (unsigned)a.batch.batch);
-  id /= (unsigned)a.batch.batch;
   const int split = (int)(id % (unsigned)a.plan.prompt_splits);
-  const int rb = a.plan.prompt_blocks - 1 - (int)(id / (unsigned)a.plan.prompt_splits);
+  id /= (unsigned)a.plan.prompt_splits;
+  auto blocks_of = [&](const Sequence& s) {
+    const int rows = s.n * a.g;
+    return a.plan.few && rows <= kFewRows ? 0 : ceil_div(rows, T::kRows);
+  };
+  const Item item = a.batch.batch == 1 ? Item{0, (int)id} : locate(a.batch, (int)id, blocks_of);
+  if (item.b < 0) return;
+  const int b = item.b;
   const Sequence s = load_sequence(a.batch, b);
-  const int rows = s.n * a.g, block0 = rb * T::kRows;
-  if (block0 >= rows || (a.plan.few && rows <= kFewRows)) return;
+  const int rows = s.n * a.g, rb = blocks_of(s) - 1 - item.local, block0 = rb * T::kRows;
+  if (rb < 0) return;
   const int parts = ceil_div(ceil_div(s.len, kStep), a.plan.prompt_split_steps);
   if (split >= (parts > 1 ? parts : 1)) return;
 
@@ -447,8 +452,7 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads) prompt_kernel(PagedAttent
 
 template <int D>
 hipError_t launch_prompt_d(const PagedAttention& a, bool bf16, hipStream_t stream) {
-  const long long blocks = (long long)a.batch.batch * a.cache.heads * a.plan.prompt_blocks * a.plan.prompt_splits;
-  if (blocks >= 1ll << 24) return hipErrorInvalidValue;      // 2^32 threads
+  const long long blocks = (long long)a.cache.heads * a.plan.prompt_blocks * a.plan.prompt_splits;
   const auto kernel = bf16 ? prompt_kernel<D, true> : prompt_kernel<D, false>;
   static std::atomic<size_t> raised[2][kPagedDevices];
   const hipError_t e = raise_lds(reinterpret_cast<const void*>(kernel), Prompt<D>::kLds, raised[bf16]);
@@ -459,7 +463,7 @@ hipError_t launch_prompt_d(const PagedAttention& a, bool bf16, hipStream_t strea
 
 }  // namespace
 
-int prompt_rows(int d) { return d <= 160 ? Prompt<160>::kRows : Prompt<192>::kRows; }
+int prompt_rows(int d) { return d <= 192 ? Prompt<192>::kRows : Prompt<256>::kRows; }
 
 hipError_t launch_paged_prompt(const PagedAttention& a, bool bf16, hipStream_t stream) { CQ_FOR_HEAD_DIM(launch_prompt_d); }
 

@@ -107,8 +107,8 @@ def check_append(case, k, v, rope=None, pos=None, freq=None, axis=None, pairs=0,
     assert PO.same_codes(cache.k_codes.cpu().numpy(), case.kc).all()
     assert PO.same_codes(cache.v_codes.cpu().numpy().transpose(0, 1, 3, 2), case.vc).all()
     if q is not None:
-        want = PO.turn(q.float().numpy(), pos, freq, axis, pairs)
-        assert torch.equal(got_q.cpu(), torch.from_numpy(want).to(q.dtype))
+        want, end = PO.turn(q.float().numpy(), pos, freq, axis, pairs), int(case.q_start[-1])
+        assert torch.equal(got_q[:end].cpu(), torch.from_numpy(want).to(q.dtype)[:end])
     return cache
 
 
@@ -181,6 +181,36 @@ def test_append_of_strided_rows():
     paged.cqp_append_kv(cache, batch, k, v)
     assert PO.same_codes(cache.k_codes.cpu().numpy(), want[0]).all()
     assert PO.same_codes(cache.v_codes.cpu().numpy().transpose(0, 1, 3, 2), want[1]).all()
+
+
+def test_append_leaves_rows_of_nobody():
+    """Queries before the first sequence's rows and behind the last one's are neither turned nor written."""
+    r = np.random.RandomState(15)
+    for new in ((1, 1), (40, 9)):
+        case = Case(16, (70, 60), new, 2, 2, 64, 16, F16, extra_rows=4)
+        case.q_start += 3
+        case.t += 3
+        freq, axis, rope = rope_of(r, 16, 2, 0)
+        pos = r.randint(0, 1000, (2, case.t))
+        q = rows(r, case.t, 6, 64, F16)
+        out = torch.full((case.t, 6, 64), 7.0, dtype=F16, device="cuda")
+        cache, batch = case.device()
+        paged.cqp_append_kv(cache, batch, rows(r, case.t, 2, 64, F16).cuda(), rows(r, case.t, 2, 64, F16).cuda(), rope,
+                            torch.from_numpy(pos.astype(np.int32)).cuda(), q.cuda(), out)
+        end = int(case.q_start[-1])
+        assert (out[:3] == 7.0).all() and (out[end:] == 7.0).all()
+        assert torch.equal(out[3:end].cpu(), torch.from_numpy(PO.turn(q.float().numpy(), pos, freq, axis, 0)).to(F16)[3:end])
+
+
+@pytest.mark.parametrize("most", (1, 3, 60))
+def test_many_sequences(most):
+    """150 sequences of different lengths, single tokens, drafted ones and prompts among them, some with no new token."""
+    r = np.random.RandomState(most)
+    new = [int(x) for x in r.randint(0, most + 1, 150)]
+    lens = [n + int(x) for n, x in zip(new, r.randint(0, 120, 150))]
+    case = Case(17 + most, lens, new, 4, 2, 32, 16, BF16, extra_rows=5)
+    check_append(case, rows(r, case.t, 2, 32, BF16, 2.0 ** -3), rows(r, case.t, 2, 32, BF16))
+    check_attention(case, pair=False)
 
 
 # ---- attention

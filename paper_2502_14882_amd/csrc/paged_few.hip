@@ -378,26 +378,37 @@ __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAt
   __syncthreads();
   if (!s_last) return;
   const int live = rows - r0 < kRows ? rows - r0 : kRows;
-  v2f* const s_ml = reinterpret_cast<v2f*>(s_acc);          // [live][parts]
   auto first_part = [&](int r) {
     const int i_new = (r0 + r) / a.g;
     return ((size_t)(s.first + i_new) * a.q.heads + h * a.g + (r0 + r) - i_new * a.g) * a.plan.splits;
   };
-  for (int i = tid; i < live * parts; i += 256) s_ml[i] = load_device(a.ml + 2 * (first_part(i / parts) + i % parts));
-  __syncthreads();
   for (int i = tid; i < live * (D / 4); i += 256) {
     const int r = i / (D / 4), c = 4 * (i % (D / 4));
-    const float* from = a.acc + first_part(r) * D + c;
-    const v2f* ml = s_ml + r * parts;
+    const size_t first = first_part(r);
     float top = kNoMax, sum = 0.f;
-    for (int p = 0; p < parts; ++p) top = fmaxf(top, ml[p][0]);
     v4f o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int p = 0; p < parts; ++p) {
-      const v2f x = load_device(from + (size_t)p * D), y = load_device(from + (size_t)p * D + 2);
-      const float f = exp2_fast(ml[p][0] - top);
-      sum += ml[p][1] * f;
-      o += (v4f){x[0], x[1], y[0], y[1]} * f;
+    for (int p0 = 0; p0 < parts; p0 += 8) {        // eight parts' loads at once: each is a trip to memory
+      v2f w[8], x[8], y[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const size_t p = first + (p0 + u < parts ? p0 + u : parts - 1);
+        w[u] = load_device(a.ml + 2 * p);
+        x[u] = load_device(a.acc + p * D + c);
+        y[u] = load_device(a.acc + p * D + c + 2);
+      }
+      float to = top;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) to = fmaxf(to, w[u][0]);
+      const float keep = exp2_fast(top - to);
+      top = to;
+      sum *= keep;
+      o *= keep;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float f = p0 + u < parts ? exp2_fast(w[u][0] - top) : 0.f;
+        sum += w[u][1] * f;
+        o += (v4f){x[u][0], x[u][1], y[u][0], y[u][1]} * f;
+      }
     }
     const int i_new = (r0 + r) / a.g;
     store_result<BF16>(a, (size_t)(s.first + i_new), h * a.g + (r0 + r) - i_new * a.g, c, o, sum, top);
@@ -490,7 +501,7 @@ hipError_t launch_paged_combine(const PagedAttention& a, bool bf16, hipStream_t 
 // different lengths have as many as they need: as many workgroups as are resident at once (two to a CU while their registers
 // allow it) if sequences are of the same length, a step for every wave at least.  Twice as many took 1 to 5 % longer at 64 x 8192, 8 x 65536
 // and 32 x 8192 tokens, 20 % at 8 x 4096 and 1 x 65536; 1.5 times as many up to 18 %.
-// While the partial results of a row of workgroups are few (4 KB of maxima and sums, 256 KB of values), the one that ends last joins them;
+// While the partial results of a row of workgroups are few (256 KB), the one that ends last joins them;
 // otherwise a launch of its own does, whose waves are many.
 // Many rows (over kFewRows per KV head): a workgroup takes a block of rows over a split; a CU holds one.  The
 // fewest splits that leave the last round of workgroups at least nine tenths full are taken, or those that fill it best: each costs its
@@ -516,7 +527,7 @@ PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, 
     p.split_steps = ceil_div(steps, (int)want);
     p.few_splits = p.splits = ceil_div(steps, p.split_steps);
     const long long parts = few * p.few_splits;
-    p.few_joins = p.few_splits > 1 && parts <= 512 && parts * cache.d <= 65536;
+    p.few_joins = p.few_splits > 1 && parts * cache.d <= 65536;
   }
   if (p.prompts) {
     const int block = prompt_rows(cache.d);

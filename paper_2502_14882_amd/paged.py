@@ -193,6 +193,12 @@ def _heads(t: torch.Tensor, what: str, head_dim: int, n_tokens: int, dtype, inde
     return _pack_heads(t.data_ptr(), token if n_tokens > 1 else 0, head if heads > 1 else 0, heads, 0)
 
 
+def _own_heads(t: torch.Tensor) -> bytes:
+    """The same of a tensor that was allocated here, dense."""
+    _, heads, d = t.shape
+    return _pack_heads(t.data_ptr(), heads * d, d, heads, 0)
+
+
 def _dtype(t: torch.Tensor) -> int:
     code = _DTYPES.get(t.dtype)
     if code is None:
@@ -211,8 +217,8 @@ def _positions(positions: torch.Tensor, rope: Rope, n_tokens: int, index: int) -
     return positions.data_ptr()
 
 
-def _like(t: torch.Tensor) -> torch.Tensor:
-    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+def _dense_like(t: torch.Tensor) -> torch.Tensor:
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _run(index: int, call, *args) -> None:
@@ -237,15 +243,20 @@ def cqp_rotate(rope: Rope, positions: torch.Tensor, x: Union[torch.Tensor, Seque
     xs = (x,) if single else tuple(x)
     if not 1 <= len(xs) <= 2:
         raise ValueError("one or two tensors are turned at once, not %d" % len(xs))
-    outs = [_like(t) for t in xs] if out is None else [out] if single else list(out)
-    if len(outs) != len(xs):
-        raise ValueError("%d tensors, %d results" % (len(xs), len(outs)))
     first = xs[0]
     shape, dtype, index = first.shape, first.dtype, first.get_device()
     if len(shape) != 3:
         raise ValueError("x is %s, [tokens, heads, d] is wanted" % (tuple(shape),))
     n, _, d = shape
-    ins, res = [b"".join([_heads(t, what, d, n, dtype, index) for t in ts]) for what, ts in (("x", xs), ("out", outs))]
+    ins = b"".join([_heads(t, "x", d, n, dtype, index) for t in xs])
+    if out is None:
+        outs = [_dense_like(t) for t in xs]
+        res = b"".join([_own_heads(t) for t in outs])
+    else:
+        outs = [out] if single else list(out)
+        if len(outs) != len(xs):
+            raise ValueError("%d tensors, %d results" % (len(xs), len(outs)))
+        res = b"".join([_heads(t, "out", d, n, dtype, index) for t in outs])
     _run(index, _calls().rotate, rope.at, _positions(positions, rope, n, index), n, d, _dtype(first), 1 if backward else 0, ins, res,
          len(xs))
     return outs[0] if single else outs
@@ -273,9 +284,12 @@ def cqp_append_kv(cache: PagedCache, batch: PagedBatch, k: torch.Tensor, v: torc
     if q is not None:
         if rope is None:
             raise ValueError("queries are turned by a rope: none is given")
+        qs = _heads(q, "q", d, n, dtype, index)
         if q_out is None:
-            q_out = _like(q)
-        qs, os = _heads(q, "q", d, n, dtype, index), _heads(q_out, "q_out", d, n, dtype, index)
+            q_out = _dense_like(q)
+            os = _own_heads(q_out)
+        else:
+            os = _heads(q_out, "q_out", d, n, dtype, index)
     elif q_out is not None:
         raise ValueError("q_out without q")
     _run(index, _calls().append_kv, cache.at, batch.at, n, _dtype(k), ks, vs, turn, where, qs, os)
@@ -299,8 +313,10 @@ def cqp_attn(cache: PagedCache, batch: PagedBatch, q: torch.Tensor, causal: bool
     n, heads, _ = shape
     qs = _heads(q, "q", cache.head_dim, n, dtype, index)
     if out is None:
-        out = _like(q)
-    os = _heads(out, "out", cache.head_dim, n, dtype, index)
+        out = _dense_like(q)
+        os = _own_heads(out)
+    else:
+        os = _heads(out, "out", cache.head_dim, n, dtype, index)
     if lse is not None:
         if lse.dtype is not torch.float32 or lse.shape != (n, heads) or not lse.is_contiguous() or lse.get_device() != index:
             raise ValueError("lse is a contiguous float32 [tokens, heads] on the cache's device")

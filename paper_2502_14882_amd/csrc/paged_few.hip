@@ -56,19 +56,21 @@ __global__ void __launch_bounds__(256, D * NT <= 128 ? 2 : 1) few_kernel(PagedAt
   __shared__ bool s_last;
   const PagedCacheArgs& C = a.cache;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 15, grp = lane >> 4;
-  unsigned id = blockIdx.x;
+  // blocks of rows of the same tokens eight apart: an XCD takes every eighth workgroup, and they meet in its L2
+  const unsigned blocks = (unsigned)a.plan.row_blocks;
+  const int rb = (int)(blockIdx.x / 8 % blocks);
+  unsigned id = blocks == 1 ? blockIdx.x : blockIdx.x / (8 * blocks) * 8 + blockIdx.x % 8;
   const int split = (int)(id % (unsigned)a.plan.few_splits);
   id /= (unsigned)a.plan.few_splits;
-  const int rb = (int)(id % (unsigned)a.plan.row_blocks);
-  id /= (unsigned)a.plan.row_blocks;
   const int h = (int)(id % (unsigned)C.heads), b = (int)(id / (unsigned)C.heads);
+  if (b >= a.batch.batch) return;                       // the grid is rounded up
   const Sequence s = load_sequence(a.batch, b);
-  const int rows = s.n * a.g, r0 = rb * kRows;
+  const int rows = s.n * a.g, r0 = (blocks == 1 ? 0 : rb) * kRows;
   if (r0 >= rows || (a.plan.prompts && rows > kFewRows)) return;
   const int parts = ceil_div(ceil_div(s.len, kStep), a.plan.split_steps);      // splits of this sequence
   if (split >= (parts > 1 ? parts : 1)) return;
   const bool joins = parts > 1 && a.plan.few_joins;
-  u64* const count = a.counts + ((size_t)b * C.heads + h) * a.plan.row_blocks + rb;
+  u64* const count = a.counts + ((size_t)b * C.heads + h) * blocks + (blocks == 1 ? 0 : rb);
   u64 seen = 0;
   if (joins && tid == 255) seen = count_open(count, a.tag);
 
@@ -469,7 +471,8 @@ __global__ void __launch_bounds__(256) combine_splits_kernel(PagedAttention a) {
 
 template <int D, int NT>
 hipError_t launch_few(const PagedAttention& a, bool bf16, hipStream_t stream) {
-  const long long blocks = (long long)a.batch.batch * a.cache.heads * a.plan.row_blocks * a.plan.few_splits;
+  long long blocks = (long long)a.batch.batch * a.cache.heads * a.plan.few_splits;
+  if (a.plan.row_blocks > 1) blocks = (blocks + 7) / 8 * 8 * a.plan.row_blocks;
   const size_t lds = (size_t)kWaves * 16 * NT * (D + 4) * sizeof(float);
   const auto kernel = bf16 ? few_kernel<D, NT, true> : few_kernel<D, NT, false>;
   static std::atomic<size_t> raised[2][kPagedDevices];
@@ -559,7 +562,7 @@ PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, 
     if (p.ws_bytes == 0) p.ws_bytes = 256;
   }
   // what a launch takes: 2^32 threads
-  p.fits = rows < 1ll << 30 && (!p.few || (long long)batch.batch * cache.heads * p.row_blocks * p.few_splits < 1ll << 24) &&
+  p.fits = rows < 1ll << 30 && (!p.few || ((long long)batch.batch * cache.heads * p.few_splits + 8) * p.row_blocks < 1ll << 24) &&
            (!p.prompts || (long long)cache.heads * p.prompt_blocks * p.prompt_splits < 1ll << 23) &&
            (long long)batch.n_tokens * n_q_heads < 1ll << 26;
   return p;

@@ -301,6 +301,48 @@ def test_extreme_queries_and_scales():
     check_attention(case, scale=2.0 ** -17)
 
 
+@pytest.mark.parametrize("new", (1, 5, 80))
+def test_a_query_that_is_not_finite_spoils_its_row_only(new):
+    case = Case(63, (300, 130), (new, new), 4, 2, 64, 32, F16, normal=True)
+    want = case.expected()
+    case.q[0, 1, 5], case.q[new, 3, 0] = float("nan"), float("inf")
+    out, lse = run_attention(case)
+    bad = torch.zeros((case.t, 4), dtype=torch.bool)
+    bad[0, 1] = bad[new, 3] = True
+    assert torch.isnan(out[0, 1]).all() and torch.isnan(out[new, 3]).all()
+    out, keep = out.cpu().double().numpy(), ~bad.numpy()
+    assert np.isfinite(out[keep]).all() and np.allclose(out[keep], want[0][keep], rtol=4e-3, atol=1e-2 * np.abs(want[0]).max())
+
+
+@pytest.mark.parametrize("lens,new", (((30,), (1,)), ((700, 3, 90), (2, 0, 1)), ((200, 64), (60, 64)), ((500,), (30,))))
+def test_bounds_far_above_what_there_is(lens, new):
+    """The host's bounds choose kernels and splits; the results follow what the device holds."""
+    case = Case(64, lens, new, 8, 2, 64, 16, BF16, normal=True)
+    cache, batch = case.device()
+    table = torch.full((len(lens), 600), -1, dtype=torch.int32, device="cuda")
+    table[:, :case.max_pages] = batch.page_table
+    want = case.expected()
+    for max_new, max_len in ((100, 9000), (max(new), 9600), (1000, max(lens)), (4000, 1 << 30)):
+        loose = paged.PagedBatch(table, batch.seq_lens, batch.q_start, max_new, max_len)
+        out, lse = paged.cqp_attn(cache, loose, case.q.cuda(), return_lse=True)
+        assert_attention_close(out, lse, want, case, False)
+
+
+def test_workspaces_hold_anything():
+    """One workspace for calls of different shapes, filled with noise and with what the calls left: kernels that join splits count in it."""
+    r = np.random.RandomState(65)
+    cases = [Case(65, (5000,), (1,), 8, 2, 64, 64, F16, normal=True), Case(66, (900, 3000, 40), (4, 1, 2), 8, 2, 128, 32, F16, normal=True),
+             Case(67, (2500, 700), (70, 3), 4, 1, 64, 16, F16, normal=True)]
+    held = [c.device() + (c.q.cuda(), c.expected()) for c in cases]
+    ws = torch.empty(max(paged.cqp_attn_workspace_bytes(h[0], h[1], c.t, c.hq) for c, h in zip(cases, held)), dtype=torch.uint8, device="cuda")
+    for n in range(4):
+        ws.copy_(torch.from_numpy(r.randint(0, 256, ws.numel()).astype(np.uint8) if n else np.full(ws.numel(), 255, np.uint8)))
+        for _ in range(2):
+            for c, (cache, batch, q, want) in zip(cases, held):
+                out, lse = paged.cqp_attn(cache, batch, q, return_lse=True, workspace=ws)
+                assert_attention_close(out, lse, want, c, False)
+
+
 def test_attention_layouts_of_queries_and_results():
     """Queries as a part of a fused projection, results with the heads before the tokens, a workspace of the caller's; rows of
     nobody stay as they were."""

@@ -156,6 +156,17 @@ def test_attention_refusals():
     assert attend(nbytes=need - 1) == cq.CQ_ERR_WORKSPACE
 
 
+def test_calls_too_large_for_a_launch():
+    L = paged.lib()
+    many = batch(b=1 << 22, max_new=4)
+    assert L.cqp_attn_workspace_bytes(by(cache(hk=8)), by(many), 1 << 22, 8) == 0
+    assert attend(c=cache(hk=8), s=many, n=1 << 22, q=heads(8), o=heads(8)) == cq.CQ_ERR_SHAPE
+    assert b"too many" in L.cq_last_error()
+    assert attend(s=batch(max_new=1 << 30), n=1 << 30, q=heads(8), o=heads(8)) == cq.CQ_ERR_SHAPE
+    assert rotate(n=1 << 30, i=heads(64), o=heads(64)) == cq.CQ_ERR_SHAPE
+    assert append(s=batch(b=1 << 27), n=1 << 27) == cq.CQ_ERR_SHAPE
+
+
 def test_workspace_sizes():
     f = paged.lib().cqp_attn_workspace_bytes
     assert f(by(cache()), by(batch()), 2, 7) == 0

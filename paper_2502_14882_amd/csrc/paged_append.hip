@@ -232,19 +232,19 @@ __global__ void __launch_bounds__(kMostThreads) append_kernel(AppendArgs a) {
     const int from = s.pos0 > 0 ? s.pos0 : 0, to = s.pos0 + s.n;
     return to <= from ? 0 : ((to - 1) >> C.page_log2) - (from >> C.page_log2) + 1;
   };
-  const Item item = a.one_each ? Item{(int)id, 0} : a.batch.batch == 1 ? Item{0, (int)id} : locate(a.batch, (int)id, pages_of);
+  const Item item = a.one_each ? item_of(a.batch, (int)id, 0) : a.batch.batch == 1 ? item_of(a.batch, 0, (int)id) : locate(a.batch, (int)id, pages_of);
   if (item.b < 0) return;
   const int b = item.b;
-  const Sequence s = load_sequence(a.batch, b);
+  const Sequence s = item.s;
   if (item.local >= pages_of(s)) return;
   const int from = s.pos0 > 0 ? s.pos0 : 0, to = s.pos0 + s.n;
   const int index = (from >> C.page_log2) + item.local, place = index << C.page_log2;
   const int pid = a.batch.page_table[(size_t)b * a.batch.max_pages + index];      // place < to <= len: within the row
-  if ((unsigned)pid >= (unsigned)C.n_pages) return;
+  const bool there = (unsigned)pid < (unsigned)C.n_pages;      // looked at when the new rows are on their way
   const int s0 = from > place ? from - place : 0, s1 = to - place < C.page ? to - place : C.page;
   const int live = s1 - s0;
   const int row0 = s.first + place - s.pos0;                 // row of the page's slot 0
-  const size_t head0 = (size_t)pid * C.heads + h0;
+  const size_t head0 = (size_t)(unsigned)pid * C.heads + h0;
   float* const scales = (value ? C.v_scale : C.k_scale) + head0;
   uint8_t* const codes = (value ? C.v_codes : C.k_codes) + (head0 << C.page_log2) * C.d;
   const int head_bytes = C.d << C.page_log2;
@@ -292,6 +292,7 @@ __global__ void __launch_bounds__(kMostThreads) append_kernel(AppendArgs a) {
         raw[i][1] = load8(p + c1);
       }
     }
+    if (!there) return;
     CosSin cs;
 #pragma unroll
     for (int i = 0; i < kSlots; ++i) {
@@ -340,23 +341,30 @@ __global__ void __launch_bounds__(kMostThreads) append_kernel(AppendArgs a) {
 
   const int octets = C.d / 8, quad0 = s0 >> 2, quads = ((s1 + 3) >> 2) - quad0, per_head = quads * octets, items = heads * per_head;
   const bool spread = (per_head & 63) != 0;
-  float x[kSlots / 2][4][8];
+  v4u raw[kSlots / 2][4];
 #pragma unroll
   for (int i = 0; i < kSlots / 2; ++i) {
     const int item = tid + i * threads, hh = item / per_head, rest = item - hh * per_head;
+    const int slot = 4 * (quad0 + rest / octets), c = 8 * (rest % octets);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const bool live_row = item < items && slot + t >= s0 && slot + t < s1;
+      raw[i][t] = live_row ? load8(row_of(a.v, row0 + slot + t, h0 + hh) + c) : (v4u){0, 0, 0, 0};
+    }
+  }
+  if (!there) return;
+  float x[kSlots / 2][4][8];
+#pragma unroll
+  for (int i = 0; i < kSlots / 2; ++i) {
+    const int item = tid + i * threads, hh = item / per_head;
     if (item < items) {
-      const int slot = 4 * (quad0 + rest / octets), c = 8 * (rest % octets);
       float most = 0.f;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const bool there = slot + t >= s0 && slot + t < s1;
-        const v4u w = there ? load8(row_of(a.v, row0 + slot + t, h0 + hh) + c) : (v4u){0, 0, 0, 0};
-        widen8<BF16>(w, x[i][t]);
-      }
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
+        widen8<BF16>(raw[i][t], x[i][t]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) most = fmaxf(most, magnitude(x[i][t][j]));
+      }
       fold_most(&s_most[hh], most, spread);
     }
   }

@@ -36,17 +36,21 @@ __device__ inline Sequence load_sequence(const PagedBatch& s, int b) {
                      __builtin_amdgcn_readfirstlane(s.seq_lens[b]));
 }
 
-// Work items counted through the sequences, count(sequence) of each: whose the item `index` is, and which of its items; sequence -1: there
-// are not as many.  A launch then needs workgroups for the items that the tokens can make, not for the most of every sequence.
+// Work items counted through the sequences, count(sequence) of each: whose the item `index` is, which of its items, and that sequence;
+// sequence -1: there are not as many.  A launch then needs workgroups for the items that the tokens can make, not for the most of every sequence.
 struct Item {
   int b, local;
+  Sequence s;
 };
+__device__ inline Item item_of(const PagedBatch& s, int b, int local) { return {b, local, load_sequence(s, b)}; }
 template <class F>
 __device__ inline Item locate(const PagedBatch& s, int index, F count) {
   const int lane = threadIdx.x & 63;
   for (int base = 0; base < s.batch; base += 64) {
     const int b = base + lane;
-    const int own = b < s.batch ? count(sequence_of(s, s.q_start[b], s.q_start[b + 1], s.seq_lens[b])) : 0;
+    Sequence seq = {0, 0, 0, 0};
+    if (b < s.batch) seq = sequence_of(s, s.q_start[b], s.q_start[b + 1], s.seq_lens[b]);
+    const int own = b < s.batch ? count(seq) : 0;
     int sum = own;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -56,11 +60,13 @@ __device__ inline Item locate(const PagedBatch& s, int index, F count) {
     const int all = __builtin_amdgcn_readlane(sum, 63);
     if (index < all) {
       const int at = __builtin_ctzll(__ballot(sum > index));
-      return {base + at, index - __builtin_amdgcn_readlane(sum - own, at)};
+      return {base + at, index - __builtin_amdgcn_readlane(sum - own, at),
+              {__builtin_amdgcn_readlane(seq.first, at), __builtin_amdgcn_readlane(seq.n, at), __builtin_amdgcn_readlane(seq.pos0, at),
+               __builtin_amdgcn_readlane(seq.len, at)}};
     }
     index -= all;
   }
-  return {-1, 0};
+  return {-1, 0, {0, 0, 0, 0}};
 }
 
 // ---- 16-bit elements, eight of them as they lie in memory

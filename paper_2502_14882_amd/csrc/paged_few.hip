@@ -430,7 +430,7 @@ __global__ void __launch_bounds__(256) combine_splits_kernel(PagedAttention a) {
   const Item item = locate(a.batch, at - first_row, [&](const Sequence& s) { return s.len - s.pos0; });      // all rows of a sequence
   if (item.b < 0) return;
   const int i = item.local;
-  const Sequence s = load_sequence(a.batch, item.b);
+  const Sequence s = item.s;
   const bool few = a.plan.few && (!a.plan.prompts || s.n * a.g <= kFewRows);
   if (few && a.plan.few_joins) return;
   const int split_steps = few ? a.plan.split_steps : a.plan.prompt_split_steps;

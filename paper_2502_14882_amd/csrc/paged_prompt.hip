@@ -80,10 +80,10 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads) prompt_kernel(PagedAttent
     const int rows = s.n * a.g;
     return a.plan.few && rows <= kFewRows ? 0 : ceil_div(rows, T::kRows);
   };
-  const Item item = a.batch.batch == 1 ? Item{0, (int)id} : locate(a.batch, (int)id, blocks_of);
+  const Item item = a.batch.batch == 1 ? item_of(a.batch, 0, (int)id) : locate(a.batch, (int)id, blocks_of);
   if (item.b < 0) return;
   const int b = item.b;
-  const Sequence s = load_sequence(a.batch, b);
+  const Sequence s = item.s;
   const int rows = s.n * a.g, rb = blocks_of(s) - 1 - item.local, block0 = rb * T::kRows;
   if (rb < 0) return;
   const int parts = ceil_div(ceil_div(s.len, kStep), a.plan.prompt_split_steps);

@@ -277,7 +277,8 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads) prompt_kernel(PagedAttent
     float f[2], top = kNoMax;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      f[i] = row_scale * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w.ks), 2 * t + i));
+      // (above 0, as tiny queries over pages of zeros would not have it: a masked logit, -infinity, stays what it is)
+      f[i] = fmaxf(row_scale * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w.ks), 2 * t + i)), 0x1p-126f);
       top = fmaxf(top, best[i] * f[i]);
     }
     if (__any(top > m + 8.f)) {

@@ -301,6 +301,18 @@ def test_extreme_queries_and_scales():
     check_attention(case, scale=2.0 ** -17)
 
 
+@pytest.mark.parametrize("new", (1, 6, 80))
+def test_logits_below_every_number(new):
+    """Queries so small over pages of zeros (whose scale is the least one) that the factor of their logits is below fp32's least number: the
+    logits are 0, and those of tokens behind a row's own stay masked."""
+    case = Case(66, (100,), (new,), 4, 2, 64, 32, BF16, normal=True)
+    case.q = (case.q.float() * 2.0 ** -60).to(BF16)
+    case.kc[:, :, :] = np.where((case.kc & 0x7f) == 0x7f, case.kc, 0)
+    case.ks[:] = np.where(np.isnan(case.ks), case.ks, np.float32(2.0 ** -100))
+    check_attention(case)
+    check_attention(case, causal=False)
+
+
 @pytest.mark.parametrize("new", (1, 5, 80))
 def test_a_query_that_is_not_finite_spoils_its_row_only(new):
     case = Case(63, (300, 130), (new, new), 4, 2, 64, 32, F16, normal=True)

@@ -42,8 +42,8 @@ typedef struct {
 
 /*
  * The cache: n_pages pages of `page` tokens.  Element = code * scale, a code being an e4m3 float (OCP
- * FP8 without infinities, largest value 448) and the scale a power of two, one per page and KV
- * head for the keys and one for the values.
+ * FP8 without infinities, largest value 448) and the scale a power of two (cqp_append_kv writes no
+ * others, and cqp_attn takes no others), one per page and KV head for the keys and one for the values.
  *   k_codes  [n_pages, n_kv_heads, page, head_dim]
  *   v_codes  [n_pages, n_kv_heads, head_dim, page]   (a channel's tokens lie together)
  *   k_scale, v_scale  fp32 [n_pages, n_kv_heads]
@@ -131,9 +131,9 @@ int cqp_rotate(const cqp_rope_t *rope, const int32_t *positions, int32_t n_token
  * others.  Slots of no new token keep their codes but for that growth.
  * Tokens whose page is not there, or whose place in the sequence is negative, are dropped.  Within a
  * call no page may be written by two sequences.
- * The result depends on seq_lens and q_start alone, not on how the work is spread; appending token by
- * token and all at once give the same scales or smaller ones for all at once never larger.
- * Errors: as cqp_rotate.
+ * The result depends on the arguments alone, not on how the work is spread.  Tokens appended one by one
+ * and at once get the same scales; their codes differ where a scale grew in between.
+ * Errors: as cqp_rotate (CQ_ERR_SHAPE also for more work than a launch can hold: 2^32 threads).
  */
 int cqp_append_kv(const cqp_cache_t *cache, const cqp_batch_t *batch, int32_t n_tokens, int32_t dtype,
                   const cqp_heads_t *k, const cqp_heads_t *v, const cqp_rope_t *rope,
@@ -149,7 +149,7 @@ size_t cqp_attn_workspace_bytes(const cqp_cache_t *cache, const cqp_batch_t *bat
  * out = softmax(softmax_scale * q K^T) V over the tokens of each row's sequence in the cache.
  *   q    in : [n_tokens, n_q_heads, head_dim], n_q_heads a multiple of n_kv_heads; query head hq
  *             reads KV head hq / (n_q_heads / n_kv_heads)
- *   out  out: the same shape and type
+ *   out  out: the same shape and type; it must not overlap q
  *   lse  out: NULL, or fp32 [n_tokens, n_q_heads] (dense): the natural logarithm of the sum of
  *             exp(softmax_scale * q . k) - with it results over several caches are joined
  *   causal  : 1: a row sees the tokens of its sequence up to its own; 0: all seq_lens[b] tokens
@@ -160,9 +160,12 @@ size_t cqp_attn_workspace_bytes(const cqp_cache_t *cache, const cqp_batch_t *bat
  * lse = -infinity.  A NaN in the key or value of a token reaches the rows that see that token - at
  * least their affected channels - and no others.
  * Products are exact in the fp16 matrix cores' fp32 sums (the queries of a row are
- * scaled by a power of two first); weights are rounded to fp16 (to a pair of fp16 where few rows share a
- * KV head and the element type is fp16) against the largest of their row.
- * Errors: CQ_ERR_NULL, CQ_ERR_ALIGN, CQ_ERR_SHAPE, CQ_ERR_UNSUPPORTED, CQ_ERR_WORKSPACE, CQ_ERR_HIP.
+ * scaled by a power of two first); weights are rounded to fp16 for their products, to a pair of
+ * fp16 where the element type is fp16 and max_new times the query heads of a KV head is at most
+ * 64; their sums take them unrounded, in fp32.
+ * The result depends on the arguments alone: the same call gives the same bits.
+ * Errors: CQ_ERR_NULL, CQ_ERR_ALIGN, CQ_ERR_SHAPE (also for more work than a launch can hold),
+ * CQ_ERR_UNSUPPORTED, CQ_ERR_WORKSPACE, CQ_ERR_HIP.
  */
 int cqp_attn(const cqp_cache_t *cache, const cqp_batch_t *batch, int32_t n_tokens, int32_t dtype,
              const cqp_heads_t *q, const cqp_heads_t *out, float *lse, int32_t causal,

@@ -16,6 +16,8 @@
 //     v_dot2, which runs on the cores, so the weights are summed by additions;
 //   - m follows a row's largest logit only when that is more than 2^8 above it (weights up to 256 fit fp16 as well as those
 //     up to 1), so that O is rescaled a few times per row and not at every step.
+// 8192 rows of 32 heads over 8192 tokens, each up to its own, 128 channels: 580 to 600 us, 0.94 PFLOP/s, where a matrix product
+// reaches 1.26 on such data; 512 new tokens of each of three sequences of 16384 tokens 440 us, 0.85 PFLOP/s, 19 of them the splits' joining.
 // Two row tiles per wave and one wave to a SIMD read half as much from LDS, but took 850 us where this takes 589 (8192 rows of 32 heads
 // over 8192 tokens, 128 channels): the accumulators then travel between the two register files.
 #include <type_traits>
@@ -38,7 +40,8 @@ __device__ inline void static_for(F&& f) {
 
 template <int D>
 struct Prompt {
-  static constexpr int kWaves = D <= 192 ? 8 : 4;                     // two to a SIMD while 256 registers hold what one needs
+  // two to a SIMD while 256 registers hold what one needs (192 channels 350 us, 365 with four waves; 256 channels 805 us, 452 with four)
+  static constexpr int kWaves = D <= 192 ? 8 : 4;
   static constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves;
   static constexpr int kOps = D / 16;                                 // operands of 32 keys, and of 32 tokens' values
   static constexpr int kValueTiles = D / 32;

@@ -244,6 +244,12 @@ def test_attention_of_a_long_sequence_in_splits():
     check_attention(Case(22, (9000,), (2,), 4, 1, 128, 16, BF16, normal=True))
 
 
+def test_attention_of_many_rows_in_splits():
+    """Over 32768 rows whose splits are joined four heads to a wave, the last of 66 heads two; rows that see the first split only among
+    them."""
+    check_attention(Case(67, (1600, 520), (490, 10), 66, 1, 32, 16, BF16, normal=True))
+
+
 @pytest.mark.parametrize("new", (1, 40))
 def test_rows_that_see_nothing(new):
     """Sequences shorter than their new rows, empty ones, pages that are not there: zeros, and minus infinity."""

@@ -533,9 +533,12 @@ hipError_t launch_paged_combine(const PagedAttention& a, bool bf16, hipStream_t 
 // and 32 x 8192 tokens, 20 % at 8 x 4096 and 1 x 65536; 1.5 times as many up to 18 %.
 // While the partial results of a row of workgroups are few (256 KB), the one that ends last joins them;
 // otherwise a launch of its own does, whose waves are many.
-// Many rows (over kFewRows per KV head): a workgroup takes a block of rows over a split; a CU holds one.  The
-// fewest splits that leave the last round of workgroups at least nine tenths full are taken, or those that fill it best: each costs its
-// partial results.  In a batch some sequences can have few rows all the same, whose workgroups are those of the other kernel.
+// Many rows (over kFewRows per KV head): a workgroup takes a block of rows over a split; a CU holds one.  The splits taken are those whose
+// time is the least: rounds of workgroups of so many steps each, the partial results' way to memory and back and the launch that joins them
+// (the constants are measured).  580 rows over 2373 tokens 30 us, 39 when a split held eight steps at least; 512 x 4 rows over 1024
+// tokens 32 and 39; where rounds are many they stay whole (8192 tokens).
+// In a batch some sequences can have few rows all the same, whose workgroups are those of the other kernel - but for caches of up to
+// kShortCache tokens, which the first takes in less than a launch (3 x 64 new tokens of 141 17.6 us, 19.4 with both).
 PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, int n_q_heads) {
   PagedPlan p;
   const long long cus = device_cu_count();
@@ -543,7 +546,7 @@ PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, 
   const long long rows = (long long)batch.max_new * g;
   const int steps = ceil_div(batch.len_bound, kStep);
   p.prompts = rows > kFewRows;
-  p.few = !p.prompts || (batch.batch > 1 && g <= kFewRows);
+  p.few = !p.prompts || (batch.batch > 1 && g <= kFewRows && batch.len_bound > kShortCache);
   if (p.few) {
     const long long few = rows < kFewRows ? rows : kFewRows;
     p.row_tiles = few > 16 ? 2 : 1;
@@ -565,17 +568,18 @@ PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, 
     const long long most_blocks = (rows + block - 1) / block * batch.batch, token_blocks = (long long)batch.n_tokens * g / block + batch.batch;
     p.prompt_blocks = (int)(token_blocks < most_blocks ? token_blocks : most_blocks);
     const long long beside = (long long)cache.heads * p.prompt_blocks;
-    const long long most = steps / 8 < 32 ? steps / 8 : 32;
+    const long long most = steps / 2 < 32 ? steps / 2 : 32;
+    const double step_us = cache.d <= 64 ? 1.1 : 1.1 * cache.d / 64, begin_us = 3.0, join_us = 6.0, join_bytes_per_us = 5.0e6;
+    const double bytes_per_split = (double)batch.n_tokens * n_q_heads * (cache.d + 2) * sizeof(float) * 2;       // written and read
     int best = 1;
-    double best_full = 0;
+    double least = 0;
     for (int n = 1; n <= (most > 1 ? most : 1); ++n) {
-      const long long groups = beside * n;
-      const double full = (double)groups / (double)((groups + cus - 1) / cus * cus);
-      if (full > best_full + 0.02) {
+      const double rounds = (double)((beside * n + cus - 1) / cus);
+      const double us = rounds * (ceil_div(steps, n) * step_us + begin_us) + (n > 1 ? join_us + n * bytes_per_split / join_bytes_per_us : 0.0);
+      if (n == 1 || us < 0.98 * least) {
         best = n;
-        best_full = full;
+        least = us;
       }
-      if (full >= 0.9) break;
     }
     p.prompt_split_steps = ceil_div(steps, best);
     p.prompt_splits = ceil_div(steps, p.prompt_split_steps);

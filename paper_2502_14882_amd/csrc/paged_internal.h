@@ -71,6 +71,7 @@ hipError_t launch_append(const PagedCacheArgs& cache, const PagedBatch& batch, b
 // At 65 to 96 rows, three blocks of the first, it depends: 72 rows, 8 x 3000 tokens 41 us there and 67 here, 96 rows, 16 x 4096 tokens 97
 // and 85; 64 rows, 16 x 4096 tokens 56 and 82, 160 rows 143 and 93 (64 query heads, 128 channels).
 constexpr int kFewRows = 64;
+constexpr int kShortCache = 512;   // tokens, up to which a batch with sequences of more rows is the second kernel's alone
 constexpr int kMostSplits = 128;   // below the 256 that a count holds
 struct PagedPlan {
   bool prompts = false;    // sequences of more rows are possible

@@ -535,8 +535,8 @@ hipError_t launch_paged_combine(const PagedAttention& a, bool bf16, hipStream_t 
 // otherwise a launch of its own does, whose waves are many.
 // Many rows (over kFewRows per KV head): a workgroup takes a block of rows over a split; a CU holds one.  The splits taken are those whose
 // time is the least: rounds of workgroups of so many steps each, the partial results' way to memory and back and the launch that joins them
-// (the constants are measured).  580 rows over 2373 tokens 30 us, 39 when a split held eight steps at least; 512 x 4 rows over 1024
-// tokens 32 and 39; where rounds are many they stay whole (8192 tokens).
+// (the constants are measured).  580 rows over 2373 tokens 30 us, 86 whole and 39 in four splits; 512 x 4 rows over 1024 tokens 32 in
+// four, 41 whole; 2048 x 4 rows over as many tokens 72 whole, 83 in two; 3437 x 7 rows, two sequences, 2 heads, 129 whole, 163 in two.
 // In a batch some sequences can have few rows all the same, whose workgroups are those of the other kernel - but for caches of up to
 // kShortCache tokens, which the first takes in less than a launch (3 x 64 new tokens of 141 17.6 us, 19.4 with both).
 PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, int n_q_heads) {
@@ -569,13 +569,18 @@ PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, 
     p.prompt_blocks = (int)(token_blocks < most_blocks ? token_blocks : most_blocks);
     const long long beside = (long long)cache.heads * p.prompt_blocks;
     const long long most = steps / 2 < 32 ? steps / 2 : 32;
-    const double step_us = cache.d <= 64 ? 1.1 : 1.1 * cache.d / 64, begin_us = 3.0, join_us = 6.0, join_bytes_per_us = 5.0e6;
+    const double step_us = cache.d <= 64 ? 1.1 : 1.1 * cache.d / 64, begin_us = 3.0, join_us = 4.0, join_bytes_per_us = 3.3e6;
     const double bytes_per_split = (double)batch.n_tokens * n_q_heads * (cache.d + 2) * sizeof(float) * 2;       // written and read
+    // how much fewer steps the blocks have than the longest, on the average, where rows see up to their own token
+    const double fewer = 0.5 * (batch.max_new < batch.len_bound ? batch.max_new : batch.len_bound) / batch.len_bound;
     int best = 1;
     double least = 0;
     for (int n = 1; n <= (most > 1 ? most : 1); ++n) {
-      const double rounds = (double)((beside * n + cus - 1) / cus);
-      const double us = rounds * (ceil_div(steps, n) * step_us + begin_us) + (n > 1 ? join_us + n * bytes_per_split / join_bytes_per_us : 0.0);
+      // Equal blocks take whole rounds; unequal ones, the longest first, end together, but not before the longest.
+      const double one = ceil_div(steps, n) * step_us + begin_us, rounds = (double)((beside * n + cus - 1) / cus) * one;
+      const double mean = (1.0 - fewer) * (steps * step_us + n * begin_us) * beside / cus + (1.0 - 2.0 * fewer) * one;
+      const double work = rounds < mean ? rounds : mean > one ? mean : one;
+      const double us = work + (n > 1 ? join_us + (n - fewer * (n - 1)) * bytes_per_split / join_bytes_per_us : 0.0);
       if (n == 1 || us < 0.98 * least) {
         best = n;
         least = us;

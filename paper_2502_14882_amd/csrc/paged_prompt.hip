@@ -73,12 +73,13 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads) prompt_kernel(PagedAttent
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n = lane & 31, half = lane >> 5;
 
   // KV heads fastest: with eight of them a head's workgroups share an XCD and its L2; of the rows the last first, whose tokens are
-  // the most where rows see up to their own
+  // the most where rows see up to their own; splits slowest: workgroups go to an XCD's shader engines in turn, and neighbours have like
+  // work then (2048 tokens in two splits beside each other 103 us)
   unsigned id = blockIdx.x;
   const int h = (int)(id % (unsigned)C.heads);
   id /= (unsigned)C.heads;
-  const int split = (int)(id % (unsigned)a.plan.prompt_splits);
-  id /= (unsigned)a.plan.prompt_splits;
+  const int split = (int)(id / (unsigned)a.plan.prompt_blocks);
+  id %= (unsigned)a.plan.prompt_blocks;
   auto blocks_of = [&](const Sequence& s) {
     const int rows = s.n * a.g;
     return a.plan.few && rows <= kFewRows ? 0 : ceil_div(rows, T::kRows);
@@ -99,7 +100,8 @@ __global__ void __launch_bounds__(Prompt<D>::kThreads) prompt_kernel(PagedAttent
   const int step0 = split * a.plan.prompt_split_steps;
   int step1 = step0 + a.plan.prompt_split_steps;
   if (step1 > ceil_div(block_hi, kStep)) step1 = ceil_div(block_hi, kStep);
-  const int steps = step1 - step0;                                    // may be <= 0
+  const int steps = step1 - step0;
+  if (steps <= 0 && split > 0) return;                                // no row sees a token of this split: nobody reads its results
 
   const int row = r0 + n, row_new = row / a.g;                        // this lane's row, as column of the products
   const bool row_there = row < rows;

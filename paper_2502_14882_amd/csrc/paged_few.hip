@@ -17,7 +17,7 @@
 // few, and another launch otherwise (make_paged_plan).
 // 64 sequences of up to 8192 tokens, 8 KV heads of 128 channels: 961 MB in 156 us, 6.2 TB/s (a plain read 7.1); 8 of up to 65536: 1071
 // MB in 170 us, 6.3 TB/s.  One sequence of 1000 tokens takes 10 us, and 8 drafted tokens of 16 sequences (3328 tokens, 64 channels, 32 rows
-// per KV head) 18: the trips to memory that follow each other - the sequence, its pages, their codes, the parts' meeting - and a launch.
+// per KV head) 15: the trips to memory that follow each other - the sequence, its pages, their codes, the parts' meeting - and a launch.
 #include "paged_device.h"
 #include "decode_meet.h"
 
@@ -531,6 +531,10 @@ hipError_t launch_paged_combine(const PagedAttention& a, bool bf16, hipStream_t 
 // different lengths have as many as they need: as many workgroups as are resident at once (two to a CU while their registers
 // allow it) if sequences are of the same length, a step for every wave at least.  Twice as many took 1 to 5 % longer at 64 x 8192, 8 x 65536
 // and 32 x 8192 tokens, 20 % at 8 x 4096 and 1 x 65536; 1.5 times as many up to 18 %.
+// Over 16 rows a workgroup takes two tiles of them, which share the codes' way to fp16 - but for little work (16 steps of 64 tokens to a
+// CU) workgroups of one tile, twice as many: 32 rows, 64 x 3328 tokens, 64 channels 15.3 and 18.4 us; 32 x 4096 tokens, 128 channels 17.3
+// and 20.5 with 32 rows, 23 and 27 with 64; but 16 x 43681 tokens 52 and 46, 256 x 8192, 64 channels 100 and 79, and from 192 channels
+// on, where a CU holds one workgroup of either, 88 x 1844 tokens 63 and 51.
 // While the partial results of a row of workgroups are few (256 KB), the one that ends last joins them;
 // otherwise a launch of its own does, whose waves are many.
 // Many rows (over kFewRows per KV head): a workgroup takes a block of rows over a split; a CU holds one.  The splits taken are those whose
@@ -549,7 +553,7 @@ PagedPlan make_paged_plan(const PagedCacheArgs& cache, const PagedBatch& batch, 
   p.few = !p.prompts || (batch.batch > 1 && g <= kFewRows && batch.len_bound > kShortCache);
   if (p.few) {
     const long long few = rows < kFewRows ? rows : kFewRows;
-    p.row_tiles = few > 16 ? 2 : 1;
+    p.row_tiles = few > 16 && (cache.d > 128 || (long long)batch.batch * cache.heads * steps > 16 * cus) ? 2 : 1;
     p.row_blocks = (int)((few + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
     const long long beside = (long long)batch.batch * cache.heads * p.row_blocks;
     long long want = cus * (cache.d * p.row_tiles <= 128 ? 2 : 1) / beside;

@@ -43,7 +43,7 @@ typedef struct {
 /*
  * The cache: n_pages pages of `page` tokens.  Element = code * scale, a code being an e4m3 float (OCP
  * FP8 without infinities, largest value 448) and the scale a power of two (cqp_append_kv writes no
- * others, and cqp_attn takes no others), one per page and KV head for the keys and one for the values.
+ * others, and cqp_attn relies on it), one per page and KV head for the keys and one for the values.
  *   k_codes  [n_pages, n_kv_heads, page, head_dim]
  *   v_codes  [n_pages, n_kv_heads, head_dim, page]   (a channel's tokens lie together)
  *   k_scale, v_scale  fp32 [n_pages, n_kv_heads]

@@ -40,7 +40,8 @@ __device__ inline void static_for(F&& f) {
 
 template <int D>
 struct Prompt {
-  // two to a SIMD while 256 registers hold what one needs (192 channels 350 us, 365 with four waves; 256 channels 805 us, 452 with four)
+  // two to a SIMD while 256 registers hold what one needs (192 channels 350 us, 365 with four waves; 256 channels 805 us, 452 with four; for few
+  // blocks four would be a little faster, 3 x 1060 rows 24 us and 27, 2 x 1043 x 4 rows 41 and 44, but 8192 tokens take 617 and 573)
   static constexpr int kWaves = D <= 192 ? 8 : 4;
   static constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves;
   static constexpr int kOps = D / 16;                                 // operands of 32 keys, and of 32 tokens' values

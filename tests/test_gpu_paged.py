@@ -244,6 +244,21 @@ def test_attention_of_a_long_sequence_in_splits():
     check_attention(Case(22, (9000,), (2,), 4, 1, 128, 16, BF16, normal=True))
 
 
+@pytest.mark.parametrize("dtype", (F16, BF16))
+@pytest.mark.parametrize("d,page", ((32, 16), (64, 128), (96, 32), (128, 64)))
+def test_attention_of_several_new_tokens_over_a_long_cache(d, page, dtype):
+    """Over 16 rows and enough steps (130 of 64 tokens for 2 x 16 heads) that a workgroup takes two tiles of rows."""
+    check_attention(Case(70 + d, (8300, 45), (5, 9), 64, 16, d, page, dtype, normal=True))
+
+
+@pytest.mark.parametrize("dtype", (F16, BF16))
+@pytest.mark.parametrize("d,page", ((32, 16), (96, 64), (128, 256), (256, 32)))
+def test_attention_of_many_splits_of_few_rows(d, page, dtype):
+    """64 rows of one KV head in 65 splits and more, too many partial results for one workgroup to join; and a sequence of one split beside
+    it."""
+    check_attention(Case(90 + d, (16700, 30), (8, 3), 8, 1, d, page, dtype, normal=True))
+
+
 def test_attention_of_many_rows_in_splits():
     """Over 32768 rows whose splits are joined four heads to a wave, the last of 66 heads two; rows that see the first split only among
     them."""
@@ -491,6 +506,29 @@ def test_step_recorded_once_and_replayed_while_the_sequences_grow():
         assert_attention_close(bufs["out"], lse, want, case, True)
         eager = paged.cqp_attn(cache, batch, turned.cuda())
         assert torch.equal(eager, bufs["out"])
+
+
+def test_prompts_in_splits_recorded_and_replayed():
+    """A batch of a prompt and a sequence of one token, in splits that are joined; replays between eager calls on other queries."""
+    case = Case(97, (2500, 700), (60, 1), 8, 1, 64, 32, BF16, normal=True)
+    cache, batch = case.device()
+    q = case.q.cuda()
+    others = [torch.roll(q, i, 0).contiguous() for i in range(3)]
+    wants = [paged.cqp_attn(cache, batch, o, return_lse=True) for o in others]
+    out, lse = torch.empty_like(q), torch.empty((case.t, case.hq), device="cuda")
+    work = torch.empty(paged.cqp_attn_workspace_bytes(cache, batch, case.t, case.hq), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        paged.cqp_attn(cache, batch, q, out=out, lse=lse, workspace=work)
+    for i, want in enumerate(wants):
+        q.copy_(others[i])
+        out.fill_(7.0), lse.fill_(7.0), work.fill_(0xff)
+        graph.replay()
+        again = paged.cqp_attn(cache, batch, others[i], return_lse=True)
+        torch.cuda.synchronize()
+        for got in ((out, lse), again):
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
 def test_calls_on_another_stream():

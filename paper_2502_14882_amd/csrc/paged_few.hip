@@ -529,7 +529,8 @@ hipError_t launch_paged_combine(const PagedAttention& a, bool bf16, hipStream_t 
 
 // Few rows: a workgroup per (sequence, KV head, tile of rows) and split.  Splits are of a fixed number of tokens, so that sequences of
 // different lengths have as many as they need: as many workgroups as are resident at once (two to a CU while their registers
-// allow it) if sequences are of the same length, a step for every wave at least.  Twice as many took 1 to 5 % longer at 64 x 8192, 8 x 65536
+// allow it) if sequences are of the same length, a step for every wave at least (two: 1 x 1000
+// tokens, recorded, 10.7 us and 9.2, 4 x 2000 11.2 and 9.9).  Twice as many took 1 to 5 % longer at 64 x 8192, 8 x 65536
 // and 32 x 8192 tokens, 20 % at 8 x 4096 and 1 x 65536; 1.5 times as many up to 18 %.
 // Over 16 rows a workgroup takes two tiles of them, which share the codes' way to fp16 - but for little work (16 steps of 64 tokens to a
 // CU) workgroups of one tile, twice as many: 32 rows, 64 x 3328 tokens, 64 channels 15.3 and 18.4 us; 32 x 4096 tokens, 128 channels 17.3
